@@ -205,7 +205,7 @@ def prepare(case, seed):
         import paper_2412_18052_b200 as gaf
         s["gaf"] = gaf
         if op in ("table_grad", "norm_grad", "weight_grad"):
-            s["workspace"] = gaf.new_layer_workspace(T, max(d, N), V=V)
+            s["workspace"] = gaf.new_layer_workspace(T, max(d, N), gaf.GAF_F32 if dtype == "f32" else gaf.GAF_BF16, V=V)
     return s
 
 
