@@ -65,18 +65,19 @@ extern "C" {
 #define GAF_MAX_BUCKETS 256     /* largest number of buckets of the bucketed variant */
 
 enum { GAF_F32 = 0, GAF_BF16 = 1 };
+enum { GAF_I32 = 0, GAF_I64 = 1 };      /* type of token numbers */
 
 enum {
     GAF_OK = 0,
     GAF_ERR_ARG = 1,            /* NULL pointer, K or D out of range, bad dtype/order/schedule */
     GAF_ERR_ALIGN = 2,          /* a device pointer is not 16-byte aligned */
-    GAF_ERR_ALIAS = 3,          /* macro_out overlaps an input gradient */
+    GAF_ERR_ALIAS = 3,          /* macro_out overlaps an input gradient; an output of a layer overlaps an input or another output */
     GAF_ERR_WORKSPACE = 4,      /* workspace missing, misaligned or too small */
     GAF_ERR_CUDA = 5,           /* a CUDA runtime call failed (launch, copy) */
     GAF_ERR_RESERVED = 6,       /* not used */
     GAF_ERR_UNSUPPORTED = 7,    /* the requested schedule cannot run for this call (K too large for it, or the
                                    device is still busy with a one-launch call on another stream) */
-    GAF_ERR_TOO_LARGE = 8       /* size beyond the fixed limit of gaf_cosdist_static */
+    GAF_ERR_TOO_LARGE = 8       /* size beyond a fixed limit: of gaf_cosdist_static, of a row of gaf_rms_norm, of a launch */
 };
 
 /* How gaf_filter_accumulate walks the K-1 sequential decisions of Algorithm 1.
@@ -371,6 +372,111 @@ int gaf_read_status(const void *workspace, void *cuda_stream, int *status_out);
 #define GAF_STATIC_MAX_D ((int64_t)1 << 31)
 int gaf_cosdist_static(const void *x, const void *y, int64_t D, int dtype,
                        float *dist_out, double *stats_out, void *cuda_stream);
+
+/*
+ * Gradients of a language model's layers, written where the filter reads them
+ * ---------------------------------------------------------------------------
+ * The calls below make micro-gradients: the layers of a language model that are bound by memory, 8-bit
+ * checkpoints of activations (K microbatches keep theirs until their backward passes), and the gradients that
+ * read them.  A weight's gradient goes straight into its slice of the flat micro-gradient that
+ * gaf_filter_accumulate takes (binary32 or bfloat16, `grad_dtype`), and is bitwise reproducible like the filter.
+ * (The paper has no counterpart: its micro-gradients come out of a training framework.)
+ *
+ *   - A matrix is T rows of d elements; `..._stride` is the distance of its rows in elements (>= d); matrices
+ *     without one are dense.  Device pointers are 16-byte aligned (a slice of a flat gradient starts at a multiple of
+ *     4 binary32 or 8 bfloat16 elements), tokens to their own size.  Any T, d, stride is taken; rows that start on
+ *     16-byte boundaries and are a multiple of 8 elements long are moved 16 bytes at a time.
+ *   - `dtype` is the type of every matrix of a call and of the norm's weight.  Elements are computed, and sums
+ *     carried, in binary32 or more, in an order that the sizes alone fix; each result is rounded once, to nearest.
+ *   - `base` (of the gradient's type, may be NULL): what is added to a weight's gradient before it is rounded, for a
+ *     weight that is used twice (an embedding table that is the output layer's weight too).  It may be the output itself.
+ *   - Outputs must not overlap inputs or one another (GAF_ERR_ALIAS) except as said.
+ *   - Infinities and NaN go through the arithmetic; nothing is screened.
+ *   - `workspace`: gaf_layer_workspace_bytes; its contents do not matter, before or between calls.  It may be the
+ *     filter's workspace if that is large enough (the layers leave alone what the filter keeps there).  Calls that share
+ *     one are ordered on one stream; graphs that are replayed at the same time need one each.
+ *     gaf_read_status tells whether a bounded wait of gaf_linear_weight_grad ran out (GAF_STATUS_TIMEOUT).
+ */
+
+/*
+ * Workspace of the layers' gradients for up to T tokens, matrices of up to `width` columns and tables of up to V rows.
+ * (dtype: GAF_F32 if any gradient call has binary32 matrices.)  Host only.
+ */
+int gaf_layer_workspace_bytes(int64_t T, int64_t width, int64_t V, int dtype, size_t *bytes_out);
+
+/*
+ * Embedding: out[t] = scale * table[tokens[t]].  A token outside 0 .. V-1 is padding: its row of `out` is zero.
+ *   table       device, V rows of d elements;  tokens  device, T numbers of `token_type`
+ *   out         device, T x d, dense
+ */
+int gaf_embedding(const void *table, int64_t table_stride, int64_t V, int64_t d, int dtype,
+                  const void *tokens, int token_type, int64_t T, double scale, void *out, void *cuda_stream);
+
+/*
+ * Its gradient: grad[v] = base[v] + scale * (sum of dy[t] over the t with tokens[t] == v, in ascending order of t, stretches of more
+ * than 32 in pieces).  Every row of `grad` is written; padding adds nothing.
+ *   dy          device, T x d;  grad  device, V x d of `grad_dtype`, dense
+ */
+int gaf_embedding_grad(const void *dy, int64_t dy_stride, int64_t T, int64_t d, int dtype,
+                       const void *tokens, int token_type, double scale, const void *base,
+                       void *grad, int grad_dtype, int64_t V,
+                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * 8-bit checkpoints.  Every 128 consecutive elements of a row (the last block of a row may be shorter) are held as e4m3 codes and
+ * one power of two: with a the largest finite magnitude, e is the smallest integer in [-120, 120] with a <= 448 * 2^e, a
+ * code is x * 2^-e rounded to nearest even, its value code * 2^e.  That value is off by at most 2^-4 of itself, or by 2^(e-10) where
+ * it is below 2^(e-6), and exact in bfloat16.  (At e = 120 codes stop at 240: no value is infinite.)  What is not finite
+ * becomes NaN and has no say in e.
+ *   codes       T rows of d bytes, rows `codes_stride` apart (a multiple of 16)
+ *   scales      T x ceil(d / 128) bytes, dense: e + 127
+ */
+int gaf_checkpoint_pack(const void *x, int64_t x_stride, int64_t T, int64_t d, int dtype,
+                        uint8_t *codes, int64_t codes_stride, uint8_t *scales, void *cuda_stream);
+int gaf_checkpoint_unpack(const uint8_t *codes, int64_t codes_stride, const uint8_t *scales, int64_t T, int64_t d,
+                          int dtype, void *out, int64_t out_stride, void *cuda_stream);
+
+/*
+ * Addition of the residual and root-mean-square norm, with 8-bit outputs:
+ *     h = x + residual (rounded to dtype; x without a residual),  r = 1 / sqrt(mean h^2 + eps),  y = h * r * weight
+ *   d           1 .. 16384 (else GAF_ERR_TOO_LARGE)
+ *   h           T x d, may be the residual's or x's own memory; NULL if not wanted; only with a residual
+ *   y           T x d or NULL
+ *   y_codes, y_scales   checkpoint of the unrounded y (what gaf_linear_weight_grad reads), or NULL
+ *   coded_y     not 0: y holds the values of its codes, so that the product that follows and that product's weight
+ *               gradient see the same numbers
+ *   h_codes, h_scales   checkpoint of h (what gaf_rms_norm_grad reads), or NULL
+ *   rstd        T floats: r, or NULL
+ */
+int gaf_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const void *weight,
+                 int64_t T, int64_t d, int dtype, double eps, void *h, void *y,
+                 uint8_t *y_codes, int64_t y_codes_stride, uint8_t *y_scales, int coded_y,
+                 uint8_t *h_codes, int64_t h_codes_stride, uint8_t *h_scales, float *rstd, void *cuda_stream);
+
+/*
+ * Its backward pass, from h or from h's checkpoint (exactly one of h and h_codes), with the r that the forward pass left:
+ *     n = h r,   dx = residual_grad + r (weight dy - n mean(weight dy n)),   dweight = base + sum over rows of dy n
+ *   dx          T x d, dense: the gradient of x and of the residual; may be dy's or residual_grad's own memory
+ *   residual_grad   gradient of h that comes past the norm, or NULL
+ *   dweight     d elements of `grad_dtype`
+ */
+int gaf_rms_norm_grad(const void *dy, int64_t dy_stride, const void *h, int64_t h_stride,
+                      const uint8_t *h_codes, int64_t h_codes_stride, const uint8_t *h_scales,
+                      const void *weight, const float *rstd, const void *residual_grad, int64_t residual_grad_stride,
+                      int64_t T, int64_t d, int dtype, void *dx, const void *base, void *dweight, int grad_dtype,
+                      void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Weight gradient of a linear layer y = x W^T from the 8-bit checkpoint of its input:
+ *     dweight[n][m] = base[n][m] + sum over t of dy[t][n] * (value of codes[t][m])
+ * on the tensor cores; binary32 dy is taken as the sum of three bfloat16 numbers (exact but for magnitudes below 2^-110).
+ *   dy          T x N; bfloat16 rows are a multiple of 8 elements apart (else GAF_ERR_ALIGN)
+ *   codes, scales   checkpoint of x, T x M;  dweight  N x M of `grad_dtype`, dense
+ */
+int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype,
+                           const uint8_t *codes, int64_t codes_stride, const uint8_t *scales,
+                           int64_t T, int64_t N, int64_t M, const void *base, void *dweight, int grad_dtype,
+                           void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* Number of kernel launches the most recent gaf_* call of this thread issued
  * (host-side counter, for benchmarks; gaf_cosdist_static counts too). */

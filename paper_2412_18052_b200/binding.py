@@ -16,6 +16,7 @@ GAF_F32, GAF_BF16 = 0, 1
 GAF_SCHED_AUTO, GAF_SCHED_STEPWISE, GAF_SCHED_GRAM, GAF_SCHED_GRAM_FUSED = 0, 1, 2, 3
 GAF_STATUS_ZERO_NORM, GAF_STATUS_NONFINITE, GAF_STATUS_TIMEOUT, GAF_STATUS_ILL_CONDITIONED = 1, 2, 4, 8
 GAF_MAX_K = 64
+GAF_CODE_BLOCK = 128                    # elements of a row that share a scale in an 8-bit checkpoint
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgaf.so")
 _lib = None
@@ -27,6 +28,8 @@ EXPORTS = [
     "gaf_filter_accumulate_any_seed", "gaf_stream_begin", "gaf_stream_push", "gaf_stream_end",
     "gaf_filter_accumulate_bucketed", "gaf_last_schedule", "gaf_last_gram_loader", "gaf_test_set_wait_fault",
     "gaf_filter_accumulate_repeat",
+    "gaf_layer_workspace_bytes", "gaf_embedding", "gaf_embedding_grad", "gaf_checkpoint_pack", "gaf_checkpoint_unpack",
+    "gaf_rms_norm", "gaf_rms_norm_grad", "gaf_linear_weight_grad",
 ]
 
 
@@ -70,6 +73,14 @@ def lib() -> ctypes.CDLL:
         L.gaf_stream_begin.argtypes = [vp, i64, i32, vp, vp, sz, vp]
         L.gaf_stream_push.argtypes = [vp, i32, i64, i32, dbl, vp, vp, sz, vp]
         L.gaf_stream_end.argtypes = [i32, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.gaf_layer_workspace_bytes.argtypes = [i64, i64, i64, i32, ctypes.POINTER(sz)]
+        L.gaf_embedding.argtypes = [vp, i64, i64, i64, i32, vp, i32, i64, dbl, vp, vp]
+        L.gaf_embedding_grad.argtypes = [vp, i64, i64, i64, i32, vp, i32, dbl, vp, vp, i32, i64, vp, sz, vp]
+        L.gaf_checkpoint_pack.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+        L.gaf_checkpoint_unpack.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, vp]
+        L.gaf_rms_norm.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, dbl, vp, vp, vp, i64, vp, i32, vp, i64, vp, vp, vp]
+        L.gaf_rms_norm_grad.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, i64, i64, i32, vp, vp, vp, i32, vp, sz, vp]
+        L.gaf_linear_weight_grad.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, vp, i32, vp, sz, vp]
         for name in EXPORTS:
             if name != "gaf_error_string":
                 getattr(L, name).restype = i32
@@ -250,6 +261,82 @@ def gaf_pairwise_cosdist(grads: Sequence[torch.Tensor], workspace: torch.Tensor,
                          gram_out: Optional[torch.Tensor] = None):
     """K x K cosine-distance matrix (float32) and Gram matrix (float64) on the device."""
     return _native().pairwise_cosdist(grads, workspace, dist_out, gram_out)
+
+
+def gaf_layer_workspace_bytes(T: int, width: int, dtype: int, V: int = 0) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().gaf_layer_workspace_bytes(T, width, V, dtype, ctypes.byref(out)), "gaf_layer_workspace_bytes")
+    return out.value
+
+
+def new_layer_workspace(T: int, width: int, dtype: int, V: int = 0, device=None) -> torch.Tensor:
+    """Workspace of the layers' gradients for up to T tokens, matrices of up to ``width`` columns and tables of V rows
+    (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter."""
+    ws = torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
+    gaf_workspace_init(ws)
+    return ws
+
+
+Checkpoint = Tuple[torch.Tensor, torch.Tensor]
+
+
+def new_checkpoint(T: int, d: int, device=None) -> Checkpoint:
+    """Room for the 8-bit checkpoint of a T x d matrix: (codes[T, d], scales[T, ceil(d / 128)]), rows of codes 16-byte aligned."""
+    codes = torch.empty(T, (d + 15) // 16 * 16, dtype=torch.uint8, device=device or "cuda")[:, :d]
+    return codes, torch.empty(T, (d + GAF_CODE_BLOCK - 1) // GAF_CODE_BLOCK, dtype=torch.uint8, device=device or "cuda")
+
+
+def gaf_embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[tokens]; tokens outside the table are padding and give zero rows.  Returns [*tokens.shape, d]."""
+    return _native().embedding(table, tokens, scale, out)
+
+
+def gaf_embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, workspace: torch.Tensor,
+                       scale: float = 1.0, base: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """grad[v] = base[v] + scale * sum of the rows of dy whose token is v, in ascending order.  ``grad`` [V, d] is a view of the
+    flat micro-gradient (float32 or bfloat16), all of which is written; ``base`` may be ``grad`` itself.  Returns grad."""
+    return _native().embedding_grad(dy, tokens, grad, workspace, scale, base)
+
+
+def gaf_checkpoint_pack(x: torch.Tensor, checkpoint: Optional[Checkpoint] = None) -> Checkpoint:
+    """8-bit checkpoint of a matrix: e4m3 codes and a power of two for every 128 elements of a row.  Returns (codes, scales)."""
+    if checkpoint is None:
+        checkpoint = new_checkpoint(x.shape[:-1].numel(), x.shape[-1], x.device)
+    return _native().checkpoint_pack(x, checkpoint)
+
+
+def gaf_checkpoint_unpack(checkpoint: Checkpoint, dtype: torch.dtype = torch.bfloat16,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of a checkpoint (exact in bfloat16 and float32)."""
+    if out is None:
+        out = torch.empty(checkpoint[0].shape, dtype=dtype, device=checkpoint[0].device)
+    return _native().checkpoint_unpack(checkpoint, out)
+
+
+def gaf_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 y: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                 y_checkpoint: Optional[Checkpoint] = None, coded_y: bool = False,
+                 h_checkpoint: Optional[Checkpoint] = None, want_y: bool = True):
+    """h = x + residual; y = h / rms(h) * weight.  Returns (y, h, rstd); h is None without a residual (it is x), y where ``want_y`` is
+    false and none is given.  ``y_checkpoint`` and ``h_checkpoint`` are filled where given; with ``coded_y`` y holds the values of its codes.
+    ``h`` may be ``residual`` or ``x`` itself."""
+    return _native().rms_norm(x, weight, residual, eps, want_y, y, h, rstd, y_checkpoint, coded_y, h_checkpoint)
+
+
+def gaf_rms_norm_grad(dy: torch.Tensor, h, weight: torch.Tensor, rstd: torch.Tensor, dweight: torch.Tensor,
+                      workspace: torch.Tensor, residual_grad: Optional[torch.Tensor] = None,
+                      dx: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None):
+    """Backward pass of gaf_rms_norm from h (a tensor, or its checkpoint) and rstd.  ``dweight`` is a view of the flat
+    micro-gradient; dx (the gradient of x and of the residual) has residual_grad added.  Returns (dx, dweight)."""
+    return _native().rms_norm_grad(dy, h, weight, rstd, dweight, workspace, residual_grad, dx, base)
+
+
+def gaf_linear_weight_grad(dy: torch.Tensor, checkpoint: Checkpoint, dweight: torch.Tensor, workspace: torch.Tensor,
+                           base: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dweight[n, m] = base[n, m] + sum over tokens of dy[t, n] * x[t, m], x the values of the checkpoint of the layer's input.
+    ``dweight`` is a view of the flat micro-gradient.  Returns dweight."""
+    return _native().linear_weight_grad(dy, checkpoint, dweight, workspace, base)
 
 
 def gaf_read_status(workspace: torch.Tensor) -> int:

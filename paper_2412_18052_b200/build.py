@@ -11,9 +11,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgaf.so")
 NATIVE = os.path.join(HERE, "_gaf_native.so")
 NATIVE_SOURCE = os.path.join(CSRC, "gaf_native.cpp")
-SOURCES = [os.path.join(CSRC, "gaf_api.cu"), os.path.join(CSRC, "gaf_static.cu")]
+OBJECTS = os.path.join(HERE, "_build")                  # one object per source, kept so that only what changed is compiled
+SOURCES = [os.path.join(CSRC, "gaf_api.cu"), os.path.join(CSRC, "gaf_layers.cu"), os.path.join(CSRC, "gaf_static.cu")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared"]
+              "-Xcompiler", "-fPIC", "-cudart", "shared"]
 
 
 def _newest_source_mtime() -> float:
@@ -26,6 +27,40 @@ def _newest_source_mtime() -> float:
 
 def _up_to_date(target: str) -> bool:
     return os.path.exists(target) and os.path.getmtime(target) >= _newest_source_mtime()
+
+
+def _object_of(source: str) -> str:
+    return os.path.join(OBJECTS, os.path.splitext(os.path.basename(source))[0] + ".o")
+
+
+def _object_up_to_date(source: str) -> bool:
+    """Whether a source's object is newer than everything that went into it (the list that nvcc left beside it)."""
+    obj = _object_of(source)
+    try:
+        with open(obj + ".d") as f:
+            parts = f.read().replace("\\\n", " ").split()
+        made = os.path.getmtime(obj)
+        return all(os.path.getmtime(p) <= made for p in parts[1:] if p != ":")
+    except OSError:
+        return False
+
+
+def _compile(force: bool, verbose: bool) -> None:
+    """Compile the sources, side by side, each to its object."""
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    os.makedirs(OBJECTS, exist_ok=True)
+    running = []
+    for source in SOURCES:
+        if not force and _object_up_to_date(source):
+            continue
+        obj, tmp = _object_of(source), _object_of(source) + f".{os.getpid()}.tmp.o"
+        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-MD", "-MF", obj + ".d", "-c", source, "-o", tmp]
+        running.append((subprocess.Popen(cmd), cmd, tmp, obj))
+    codes = [p.wait() for p, _, _, _ in running]
+    for rc, (_, cmd, tmp, obj) in zip(codes, running):
+        if rc != 0:
+            raise subprocess.CalledProcessError(rc, cmd)
+        os.replace(tmp, obj)
 
 
 def _native_command(out: str) -> list:
@@ -44,10 +79,10 @@ def _native_command(out: str) -> list:
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile ``libgaf.so`` and ``_gaf_native.so`` next to this file if they are missing or out of date."""
     if force or not _up_to_date(LIB):
+        _compile(force, verbose)
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
         tmp = LIB + f".{os.getpid()}.tmp"
-        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
-        subprocess.check_call(cmd)
+        subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared", "-o", tmp] + [_object_of(s) for s in SOURCES])
         os.replace(tmp, LIB)
     if force or not _up_to_date(NATIVE):
         tmp = NATIVE + f".{os.getpid()}.tmp"

@@ -37,6 +37,10 @@ static_assert(sizeof(Control) <= kControlBytes, "control block");
 constexpr size_t kPartialsOffset = kControlBytes;
 constexpr size_t kPartialsBytes = size_t(kMaxCtas) * 3 * sizeof(double);
 constexpr size_t kExtraOffset = kPartialsOffset + kPartialsBytes;
+// The scratch of the layers' gradients starts behind everything that a filter call expects to find as the call before left it, so
+// that one workspace can serve both.
+constexpr size_t kLayerScratchOffset = kExtraOffset + (size_t(148) << 10);
+static_assert(kLayerScratchOffset % 256 == 0, "workspace layout");
 
 // ------------------------------------------------------------- election ----
 

@@ -10,10 +10,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <new>
 #include <vector>
 
 #include "../../include/gaf.h"
@@ -333,6 +335,319 @@ PyObject *py_stream_end(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- layers of a language model -----------------------------------------------------------------------------------
+
+[[noreturn]] void fail_value(const char *what, const char *text) {
+    PyErr_Format(PyExc_ValueError, "%s %s", what, text);
+    throw Failed();
+}
+// A tensor on the current device, whose stream the call will use.
+const at::Tensor &cuda_tensor(PyObject *o, const char *what) {
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || t.device().index() != c10::cuda::current_device()) fail_value(what, "must be on the current CUDA device");
+    return t;
+}
+int float_code(const at::Tensor &t, const char *what) {
+    if (t.scalar_type() == at::kFloat) return GAF_F32;
+    if (t.scalar_type() == at::kBFloat16) return GAF_BF16;
+    PyErr_Format(PyExc_TypeError, "%s must be float32 or bfloat16, got %s", what, c10::toString(t.scalar_type()));
+    throw Failed();
+}
+at::ScalarType float_type(int code) { return code == GAF_F32 ? at::kFloat : at::kBFloat16; }
+
+// Rows of elements next to one another: any leading dimensions that are laid out as one (a missing matrix: null).
+struct Matrix {
+    void *ptr = nullptr;
+    int64_t rows = 0, cols = 0, stride = 0;
+    int dtype = 0;
+    const at::Tensor *t = nullptr;
+    Matrix() = default;
+    Matrix(PyObject *o, const char *what, at::ScalarType want = at::ScalarType::Undefined) {
+        if (o == Py_None) return;
+        t = &cuda_tensor(o, what);
+        if (want == at::ScalarType::Undefined) dtype = float_code(*t, what);
+        else if (t->scalar_type() != want) {
+            PyErr_Format(PyExc_TypeError, "%s must be %s, got %s", what, c10::toString(want), c10::toString(t->scalar_type()));
+            throw Failed();
+        }
+        if (t->dim() < 1) fail_value(what, "must have rows");
+        const int64_t n = t->dim();
+        cols = t->size(n - 1);
+        rows = 1;
+        stride = cols;
+        bool any = false;                // whether a dimension longer than 1 has set the stride
+        for (int64_t i = n - 2; i >= 0; --i) {
+            if (t->size(i) != 1) {
+                if (!any) { stride = t->stride(i); any = true; }
+                else if (t->numel() > 0 && t->stride(i) != stride * rows) fail_value(what, "must have rows at equal distances");
+            }
+            rows *= t->size(i);
+        }
+        if (cols > 1 && t->stride(n - 1) != 1) fail_value(what, "must have rows of neighbouring elements");
+        ptr = t->data_ptr();
+    }
+    bool has(int64_t r, int64_t c) const { return rows == r && cols == c; }
+};
+void same_shape(const Matrix &m, int64_t rows, int64_t cols, int dtype, const char *what) {
+    if (m.t && (!m.has(rows, cols) || m.dtype != dtype)) fail_value(what, "has another shape or type than the call's matrices");
+}
+// A vector, or a block of memory that is used as one.
+const at::Tensor &dense(PyObject *o, const char *what, int64_t numel) {
+    const at::Tensor &t = cuda_tensor(o, what);
+    if (!t.is_contiguous() || t.numel() != numel) fail_value(what, "must be contiguous and of the right size");
+    return t;
+}
+// An output that is given (dense, of this size and type) or made; `like`: the shape that a new one takes.
+struct LayerOutput {
+    PyObject *object = nullptr;
+    void *ptr = nullptr;
+    LayerOutput() = default;
+    LayerOutput(PyObject *given, at::IntArrayRef shape, at::ScalarType type, at::Device device, const char *what) {
+        if (given != Py_None) {
+            int64_t n = 1;
+            for (int64_t s : shape) n *= s;
+            const at::Tensor &t = dense(given, what, n);
+            if (t.scalar_type() != type || t.dim() < 1 || t.size(t.dim() - 1) != shape.back()) fail_value(what, "has another shape or type than the result");
+            ptr = t.data_ptr();
+            object = Py_NewRef(given);
+        } else {
+            const at::Tensor t = at::empty(shape, at::TensorOptions().dtype(type).device(device));
+            ptr = t.data_ptr();
+            object = THPVariable_Wrap(t);
+            if (!object) throw Failed();
+        }
+    }
+    ~LayerOutput() { Py_XDECREF(object); }
+    LayerOutput(const LayerOutput &) = delete;
+    PyObject *take() {
+        PyObject *o = object ? object : Py_NewRef(Py_None);
+        object = nullptr;
+        return o;
+    }
+};
+// Codes and scales of a matrix of `rows` x `cols`: a pair of uint8 tensors, or None.
+struct Checkpoint {
+    Matrix codes;
+    uint8_t *scales = nullptr;
+    Checkpoint(PyObject *o, const char *what, int64_t rows = -1, int64_t cols = -1) {
+        if (o == Py_None) return;
+        const Sequence seq(o, true);
+        if (seq.n != 2) fail_value(what, "is a pair of codes and scales");
+        codes = Matrix(seq[0], what, at::kByte);
+        if (rows < 0) { rows = codes.rows; cols = codes.cols; }
+        if (!codes.has(rows, cols)) fail_value(what, "has another shape than the call's matrices");
+        const at::Tensor &s = dense(seq[1], what, rows * ((cols + 127) / 128));
+        if (s.scalar_type() != at::kByte) fail_value(what, "has scales that are not uint8");
+        scales = static_cast<uint8_t *>(s.data_ptr());
+    }
+    uint8_t *ptr() const { return static_cast<uint8_t *>(codes.ptr); }
+};
+struct Tokens {
+    const void *ptr;
+    int64_t n;
+    int type;
+    const at::Tensor &t;
+    explicit Tokens(PyObject *o) : t(cuda_tensor(o, "tokens")) {
+        if (t.scalar_type() == at::kLong) type = GAF_I64;
+        else if (t.scalar_type() == at::kInt) type = GAF_I32;
+        else fail(PyExc_TypeError, "tokens must be int64 or int32");
+        if (!t.is_contiguous()) fail_value("tokens", "must be contiguous");
+        ptr = t.data_ptr();
+        n = t.numel();
+    }
+};
+struct LayerWorkspace {
+    void *ptr;
+    size_t bytes;
+    explicit LayerWorkspace(PyObject *o) {
+        const at::Tensor &t = cuda_tensor(o, "workspace");
+        if (!t.is_contiguous()) fail_value("workspace", "must be contiguous");
+        ptr = t.data_ptr();
+        bytes = t.nbytes();
+    }
+};
+// The gradient of a weight (any dense view of a flat gradient) and what is added to it.
+struct WeightGradient {
+    void *ptr;
+    const void *base = nullptr;
+    int dtype;
+    PyObject *object;
+    WeightGradient(PyObject *grad, PyObject *base_o, int64_t numel, const char *what) : object(grad) {
+        const at::Tensor &t = dense(grad, what, numel);
+        dtype = float_code(t, what);
+        ptr = t.data_ptr();
+        if (base_o != Py_None) {
+            const at::Tensor &b = dense(base_o, "base", numel);
+            if (b.scalar_type() != t.scalar_type()) fail_value("base", "has another type than the gradient");
+            base = b.data_ptr();
+        }
+    }
+};
+std::vector<int64_t> shape_with(const at::Tensor &like, bool drop_last, int64_t last) {
+    std::vector<int64_t> s(like.sizes().begin(), like.sizes().end());
+    if (drop_last) s.pop_back();
+    if (last >= 0) s.push_back(last);
+    return s;
+}
+
+PyObject *py_embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 4, [&] {
+        const Matrix table(a[0], "table");
+        if (!table.t || table.t->dim() != 2) fail_value("table", "must be a matrix");
+        const Tokens tokens(a[1]);
+        const double scale = number(a[2]);
+        const std::vector<int64_t> shape = shape_with(tokens.t, false, table.cols);
+        LayerOutput out(a[3], shape, table.t->scalar_type(), table.t->device(), "out");
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_embedding(table.ptr, table.stride, table.rows, table.cols, table.dtype, tokens.ptr, tokens.type, tokens.n, scale, out.ptr, st);
+        }), "gaf_embedding");
+        return out.take();
+    });
+}
+
+PyObject *py_embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 6, [&] {
+        const Matrix dy(a[0], "dy");
+        if (!dy.t) fail_value("dy", "is missing");
+        const Tokens tokens(a[1]);
+        if (tokens.n != dy.rows) fail_value("tokens", "must be one per row of dy");
+        const at::Tensor &grad = cuda_tensor(a[2], "grad");
+        if (grad.dim() != 2 || grad.size(1) != dy.cols) fail_value("grad", "must be a matrix as wide as dy");
+        const WeightGradient g(a[2], a[5], grad.numel(), "grad");
+        const LayerWorkspace ws(a[3]);
+        const double scale = number(a[4]);
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_embedding_grad(dy.ptr, dy.stride, dy.rows, dy.cols, dy.dtype, tokens.ptr, tokens.type, scale, g.base, g.ptr, g.dtype, grad.size(0),
+                                      ws.ptr, ws.bytes, st);
+        }), "gaf_embedding_grad");
+        return Py_NewRef(a[2]);
+    });
+}
+
+PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        // x, weight, residual, eps, want_y, y, h, rstd, y_checkpoint, coded_y, h_checkpoint
+        const Matrix x(a[0], "x");
+        if (!x.t) fail_value("x", "is missing");
+        const at::Tensor &weight = dense(a[1], "weight", x.cols);
+        if (weight.scalar_type() != x.t->scalar_type()) fail_value("weight", "has another type than x");
+        const Matrix residual(a[2], "residual");
+        same_shape(residual, x.rows, x.cols, x.dtype, "residual");
+        const double eps = number(a[3]);
+        const bool want_y = PyObject_IsTrue(a[4]) == 1, coded_y = PyObject_IsTrue(a[9]) == 1;
+        const std::vector<int64_t> shape = shape_with(*x.t, false, -1), rows = shape_with(*x.t, true, -1);
+        const at::ScalarType type = x.t->scalar_type();
+        const at::Device device = x.t->device();
+        LayerOutput y, h, rstd;
+        auto make = [&](LayerOutput &o, PyObject *given, const char *what) { new (&o) LayerOutput(given, shape, type, device, what); };
+        if (want_y || a[5] != Py_None) make(y, a[5], "y");
+        if (residual.t) make(h, a[6], "h");
+        else if (a[6] != Py_None) fail_value("h", "is only written with a residual");
+        if (a[7] != Py_None) {
+            const at::Tensor &t = dense(a[7], "rstd", x.rows);
+            if (t.scalar_type() != at::kFloat) fail_value("rstd", "must be float32");
+            rstd.ptr = t.data_ptr();
+            rstd.object = Py_NewRef(a[7]);
+        } else {
+            const at::Tensor t = at::empty(rows, at::TensorOptions().dtype(at::kFloat).device(device));
+            rstd.ptr = t.data_ptr();
+            rstd.object = THPVariable_Wrap(t);
+            if (!rstd.object) throw Failed();
+        }
+        const Checkpoint yc(a[8], "y_checkpoint", x.rows, x.cols), hc(a[10], "h_checkpoint", x.rows, x.cols);
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_rms_norm(x.ptr, x.stride, residual.ptr, residual.stride, weight.data_ptr(), x.rows, x.cols, x.dtype, eps, h.ptr, y.ptr, yc.ptr(),
+                                yc.codes.stride, yc.scales, coded_y, hc.ptr(), hc.codes.stride, hc.scales, static_cast<float *>(rstd.ptr), st);
+        }), "gaf_rms_norm");
+        return tuple_of(y, h, rstd);
+    });
+}
+
+PyObject *py_rms_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 9, [&] {
+        // dy, h (a matrix or a checkpoint), weight, rstd, dweight, workspace, residual_grad, dx, base
+        const Matrix dy(a[0], "dy");
+        if (!dy.t) fail_value("dy", "is missing");
+        const bool coded = PyTuple_Check(a[1]) || PyList_Check(a[1]);
+        const Matrix h(coded ? Py_None : a[1], "h");
+        if (!coded && !h.t) fail_value("h", "is missing");
+        const Checkpoint hc(coded ? a[1] : Py_None, "h", dy.rows, dy.cols);
+        same_shape(h, dy.rows, dy.cols, dy.dtype, "h");
+        const at::Tensor &weight = dense(a[2], "weight", dy.cols);
+        if (weight.scalar_type() != dy.t->scalar_type()) fail_value("weight", "has another type than dy");
+        const at::Tensor &rstd = dense(a[3], "rstd", dy.rows);
+        if (rstd.scalar_type() != at::kFloat) fail_value("rstd", "must be float32");
+        const WeightGradient g(a[4], a[8], dy.cols, "dweight");
+        const LayerWorkspace ws(a[5]);
+        const Matrix residual_grad(a[6], "residual_grad");
+        same_shape(residual_grad, dy.rows, dy.cols, dy.dtype, "residual_grad");
+        const std::vector<int64_t> shape = shape_with(*dy.t, false, -1);
+        LayerOutput dx(a[7], shape, dy.t->scalar_type(), dy.t->device(), "dx");
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_rms_norm_grad(dy.ptr, dy.stride, h.ptr, h.stride, hc.ptr(), hc.codes.stride, hc.scales, weight.data_ptr(),
+                                     static_cast<const float *>(rstd.data_ptr()), residual_grad.ptr, residual_grad.stride, dy.rows, dy.cols, dy.dtype, dx.ptr,
+                                     g.base, g.ptr, g.dtype, ws.ptr, ws.bytes, st);
+        }), "gaf_rms_norm_grad");
+        PyObject *const r = PyTuple_New(2);
+        if (!r) throw Failed();
+        PyTuple_SET_ITEM(r, 0, dx.take());
+        PyTuple_SET_ITEM(r, 1, Py_NewRef(a[4]));
+        return r;
+    });
+}
+
+PyObject *py_checkpoint_pack(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 2, [&] {
+        const Matrix x(a[0], "x");
+        if (!x.t) fail_value("x", "is missing");
+        const Checkpoint c(a[1], "checkpoint", x.rows, x.cols);
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_checkpoint_pack(x.ptr, x.stride, x.rows, x.cols, x.dtype, c.ptr(), c.codes.stride, c.scales, st);
+        }), "gaf_checkpoint_pack");
+        return Py_NewRef(a[1]);
+    });
+}
+
+PyObject *py_checkpoint_unpack(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 2, [&] {
+        const Checkpoint c(a[0], "checkpoint");
+        const Matrix out(a[1], "out");
+        if (!out.t || !out.has(c.codes.rows, c.codes.cols)) fail_value("out", "has another shape than the checkpoint");
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_checkpoint_unpack(c.ptr(), c.codes.stride, c.scales, out.rows, out.cols, out.dtype, out.ptr, out.stride, st);
+        }), "gaf_checkpoint_unpack");
+        return Py_NewRef(a[1]);
+    });
+}
+
+PyObject *py_linear_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 5, [&] {
+        // dy, checkpoint, dweight, workspace, base
+        const Matrix dy(a[0], "dy");
+        if (!dy.t) fail_value("dy", "is missing");
+        const Checkpoint c(a[1], "checkpoint");
+        if (!c.codes.t) fail_value("checkpoint", "is missing");
+        if (c.codes.rows != dy.rows) fail_value("checkpoint", "must have as many rows as dy");
+        const at::Tensor &dweight = cuda_tensor(a[2], "dweight");
+        if (dweight.dim() != 2 || dweight.size(0) != dy.cols || dweight.size(1) != c.codes.cols)
+            fail_value("dweight", "must be a matrix of dy's columns by the checkpoint's");
+        const WeightGradient g(a[2], a[4], dweight.numel(), "dweight");
+        const LayerWorkspace ws(a[3]);
+        void *const st = stream();
+        check(without_gil([&] {
+            return gaf_linear_weight_grad(dy.ptr, dy.stride, dy.dtype, c.ptr(), c.codes.stride, c.scales, dy.rows, dy.cols, c.codes.cols, g.base, g.ptr, g.dtype,
+                                          ws.ptr, ws.bytes, st);
+        }), "gaf_linear_weight_grad");
+        return Py_NewRef(a[2]);
+    });
+}
+
 PyObject *py_register_error(PyObject *, PyObject *cls) {
     Py_XSETREF(g_error, Py_NewRef(cls));
     return Py_NewRef(Py_None);
@@ -342,6 +657,8 @@ PyObject *py_register_error(PyObject *, PyObject *cls) {
 PyMethodDef methods[] = {
     FAST(filter_accumulate), FAST(filter_accumulate_any_seed), FAST(filter_accumulate_bucketed), FAST(pairwise_cosdist),
     FAST(cosdist), FAST(stream_begin), FAST(stream_push), FAST(stream_end),
+    FAST(embedding), FAST(embedding_grad), FAST(rms_norm), FAST(rms_norm_grad), FAST(checkpoint_pack), FAST(checkpoint_unpack),
+    FAST(linear_weight_grad),
     {"register_error", py_register_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
