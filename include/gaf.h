@@ -470,7 +470,7 @@ int gaf_rms_norm_grad(const void *dy, int64_t dy_stride, const void *h, int64_t 
  * Weight gradient of a linear layer y = x W^T from the 8-bit checkpoint of its input:
  *     dweight[n][m] = base[n][m] + sum over t of dy[t][n] * (value of codes[t][m])
  * on the tensor cores; binary32 dy is taken as the sum of three bfloat16 numbers (exact but for magnitudes below 2^-110).
- *   dy          T x N; bfloat16 rows are a multiple of 8 elements apart (else GAF_ERR_ALIGN)
+ *   dy          T x N; bfloat16 rows that are a multiple of 8 elements apart are read in place, others laid out anew first
  *   codes, scales   checkpoint of x, T x M;  dweight  N x M of `grad_dtype`, dense
  */
 int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype,

@@ -135,11 +135,12 @@ WgPlan weight_grad_plan(int64_t T, int64_t N, int64_t M, int dtype, int64_t sms)
     return p;
 }
 struct WgLayout { size_t partials, terms, end; };
-WgLayout weight_grad_layout(const WgPlan &p, int64_t N, int64_t M, int dtype) {
+// `relaid`: matrices that dy is laid out anew as.
+WgLayout weight_grad_layout(const WgPlan &p, int64_t N, int64_t M, int relaid) {
     WgLayout l{};
     l.partials = kLayerScratchOffset;
     l.terms = l.partials + (p.splits > 1 ? round_up(size_t(p.splits) * size_t(N) * size_t(M) * 4, 256) : 0);
-    l.end = l.terms + (dtype == GAF_F32 ? round_up(size_t(3) * size_t(p.steps_per_term) * kWgK * round_up(size_t(N), 8) * 2, 256) : 0);
+    l.end = l.terms + round_up(size_t(relaid) * size_t(p.steps_per_term) * kWgK * round_up(size_t(N), 8) * 2, 256);
     return l;
 }
 
@@ -272,7 +273,7 @@ int gaf_layer_workspace_bytes(int64_t T, int64_t width, int64_t V, int dtype, si
     const int64_t tiles = std::min(kWgMaxSplitItems, ceil_div(width, kWgM) * ceil_div(width, kWgN) *
                                                                ceil_div(ceil_div(T, kWgK) * (dtype == GAF_F32 ? 3 : 1), kWgChunkSteps));
     size_t wg = kLayerScratchOffset + size_t(tiles) * kWgM * kWgN * 4 + 256;
-    if (dtype == GAF_F32) wg += size_t(3) * round_up(size_t(T), kWgK) * round_up(size_t(width), 8) * 2;
+    wg += size_t(dtype == GAF_F32 ? 3 : 1) * round_up(size_t(T), kWgK) * round_up(size_t(width), 8) * 2;
     const size_t a = embed_layout(T, width, V).end, b = norm_grad_bytes(width);
     *bytes_out = round_up(std::max(wg, std::max(a, b)), 256);
     return GAF_OK;
@@ -443,8 +444,8 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     GAF_TRY(check_matrix(dweight, N, M, M));
     if (!aligned16(base)) return GAF_ERR_ALIGN;
     if (N == 0 || M == 0) return GAF_OK;
-    // (tensor copies of bfloat16 rows start on 16-byte boundaries; binary32 rows are read element by element)
-    if (dtype == GAF_BF16 && T > 1 && dy_stride % 8 != 0) return GAF_ERR_ALIGN;
+    // tensor copies read bfloat16 rows that start on 16-byte boundaries; everything else is laid out anew
+    const int relaid = dtype == GAF_F32 ? 3 : (T > 1 && dy_stride % 8 != 0 ? 1 : 0);
     const size_t ge = elem_bytes(grad_dtype);
     const Span o(dweight, N, M, M, ge), b(base, N, M, M, ge);
     if (o.meets(Span(dy, T, N, dy_stride, elem_bytes(dtype))) || o.meets(Span(codes, T, M, codes_stride, 1)) ||
@@ -454,7 +455,7 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     // (a device with more SMs than the workspace was laid out for would split no further)
     const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms, kWgMaxSplitItems));
     if (p.steps * kWgK > kMaxRows) return GAF_ERR_TOO_LARGE;
-    const WgLayout l = weight_grad_layout(p, N, M, dtype);
+    const WgLayout l = weight_grad_layout(p, N, M, relaid);
     GAF_TRY(check_workspace(workspace, workspace_bytes, l.end));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     int launches = 0;
@@ -473,9 +474,9 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     if (T > 0) {
         const void *y = dy;
         int64_t y_rows = T, y_pitch = (T > 1 ? dy_stride : int64_t(round_up(size_t(N), 8))) * 2;
-        if (dtype == GAF_F32) {
+        if (relaid) {
             WgTermsArgs t{};
-            t.dy = static_cast<const float *>(dy); t.out = in_workspace<__nv_bfloat16>(workspace, l.terms);
+            t.dy = dy; t.out = in_workspace<__nv_bfloat16>(workspace, l.terms);
             t.stride = dy_stride; t.T = T; t.N = N; t.rows = p.steps_per_term * kWgK; t.pitch = int64_t(round_up(size_t(N), 8));
             cudaLaunchConfig_t cfg{};
             cfg.gridDim = dim3(unsigned(ceil_div(t.pitch, 256)), unsigned(std::min<int64_t>(t.rows, 65535)));
@@ -485,10 +486,11 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
             attr[0].val.programmaticStreamSerializationAllowed = 1;
             cfg.attrs = attr; cfg.numAttrs = 1;
-            const cudaError_t err = cudaLaunchKernelEx(&cfg, weight_grad_terms_kernel, t);
+            const cudaError_t err = dtype == GAF_F32 ? cudaLaunchKernelEx(&cfg, weight_grad_terms_kernel<float>, t)
+                                                     : cudaLaunchKernelEx(&cfg, weight_grad_terms_kernel<__nv_bfloat16>, t);
             ++launches;
             if (err != cudaSuccess) return launched(err, launches);
-            y = t.out; y_rows = 3 * t.rows; y_pitch = t.pitch * 2;
+            y = t.out; y_rows = relaid * t.rows; y_pitch = t.pitch * 2;
         }
         if (!matrix_map(&dy_map, y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, N, y_rows, y_pitch, 64, kWgK, CU_TENSOR_MAP_SWIZZLE_128B) ||
             !matrix_map(&code_map, codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, M, T, T > 1 ? codes_stride : int64_t(round_up(size_t(M), 16)),

@@ -372,24 +372,28 @@ __global__ void __launch_bounds__(256) weight_grad_join_kernel(const WgJoinArgs 
     for (int i = 0; i < n; ++i) out[e0 + i] = from_float<G>(base ? v[i] + to_float<G>(base[e0 + i]) : v[i]);
 }
 
-// Binary32 dy as three bfloat16 matrices that add up to it: dy = hi + mid + lo, each the rest rounded to nearest (8 bits a time;
-// exact while no term is below bfloat16's subnormals).  Term k is rows k * rows .. + T of `out`; the rows from T on are zero.
+// dy laid out anew where tensor copies cannot read it as it is, as matrices below one another whose rows start on 16-byte boundaries.
+// Binary32 as three bfloat16 matrices that add up to it: dy = hi + mid + lo, each the rest rounded to nearest (8 bits a time; exact
+// while no term is below bfloat16's subnormals); bfloat16 rows at other distances as one.  Term k is rows k * rows .. + T of `out`; the
+// rows from T on are zero.
 struct WgTermsArgs {
-    const float *dy;
+    const void *dy;
     __nv_bfloat16 *out;
     int64_t stride, T, N, rows, pitch;
 };
+template <typename T>
 __global__ void __launch_bounds__(256) weight_grad_terms_kernel(const WgTermsArgs a) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
+    constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     grid_wait();
     if (c >= a.pitch) return;
-    for (int64_t row = t; row < a.rows; row += gridDim.y) {
-        float x = row < a.T && c < a.N ? a.dy[row * a.stride + c] : 0.f;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        float x = row < a.T && c < a.N ? to_float<T>(static_cast<const T *>(a.dy)[row * a.stride + c]) : 0.f;
         const bool finite = (__float_as_uint(x) & 0x7FFFFFFFu) < kInfBits;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < kTerms; ++k) {
             // (near the largest binary32 number the nearest bfloat16 is infinite: the largest finite one leaves a rest that still fits)
-            float h = __bfloat162float(__float2bfloat16_rn(x));
+            float h = rounded<__nv_bfloat16>(x);
             if (finite && (__float_as_uint(h) & 0x7FFFFFFFu) >= kInfBits) h = copysignf(__uint_as_float(0x7F7F0000u), x);
             a.out[(k * a.rows + row) * a.pitch + c] = __float2bfloat16_rn(h);
             x = finite ? x - h : 0.f;

@@ -111,7 +111,7 @@ def test_linear_weight_grad_refusals(L):
     assert call(N=0) == OK and call(M=0) == OK
     assert call(dy=None) == ARG and call(codes=None) == ARG and call(scales=None) == ARG and call(dw=None) == ARG
     assert call(ds=63) == ARG and call(cs=112) == ARG and call(dtype=2) == ARG and call(gt=2) == ARG and call(T=-1) == ARG and call(N=-1) == ARG
-    assert call(ds=68) == ALIGN and call(cs=136) == ALIGN and call(dy=A + 8) == ALIGN and call(base=A + 5 * G + 4) == ALIGN
+    assert call(cs=136) == ALIGN and call(dy=A + 8) == ALIGN and call(base=A + 5 * G + 4) == ALIGN
     assert call(dw=A) == ALIAS and call(dw=A + G + 16) == ALIAS and call(base=A + 3 * G + 16) == ALIAS
 
 
