@@ -94,7 +94,7 @@ int by_width(int64_t d, F &&f) {
 // ---------------------------------------------------------------- workspace --
 
 constexpr int kNormMaxCtas = 592;                       // rows of partial sums for the norm weight's gradient
-constexpr int64_t kWgMaxSplitItems = 296;               // most work items of a weight gradient whose tokens are split
+constexpr int64_t kWgMaxSplitItems = 148;               // most work items (pairs of CTAs) of a weight gradient whose tokens are split
 
 struct EmbedLayout { size_t cursors, count, start, slot, pos, ordered, heavy, piece, partials, end; };
 EmbedLayout embed_layout(int64_t T, int64_t d, int64_t V) {
@@ -124,10 +124,10 @@ WgPlan weight_grad_plan(int64_t T, int64_t N, int64_t M, int dtype, int64_t sms)
     WgPlan p{};
     p.steps_per_term = ceil_div(T, kWgK);
     p.steps = p.steps_per_term * (dtype == GAF_F32 ? 3 : 1);
-    p.tiles_m = ceil_div(M, kWgM);
+    p.tiles_m = ceil_div(M, kWgPairM);
     p.tiles_n = ceil_div(N, kWgN);
     const int64_t chains = ceil_div(p.steps, kWgChunkSteps), tiles = p.tiles_m * p.tiles_n;
-    int64_t splits = tiles > 0 ? sms / tiles : 1;
+    int64_t splits = tiles > 0 ? sms / 2 / tiles : 1;
     if (splits > chains) splits = chains;
     if (splits < 1) splits = 1;
     p.steps_per_split = ceil_div(chains, splits) * kWgChunkSteps;
@@ -256,8 +256,7 @@ int launch_weight_grad_tiles(const WeightGradArgs &w, const CUtensorMap &dy_map,
         return cudaFuncSetAttribute(weight_grad_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.dyn) == cudaSuccess ? int(GAF_OK)
                                                                                                                           : int(GAF_ERR_CUDA);
     }));
-    const int64_t items = w.tiles_m * w.tiles_n * w.splits;
-    const int grid = int(std::min<int64_t>(items, di.sms));
+    const int grid = 2 * std::min(w.items, di.sms / 2);
     const cudaError_t err = launch_dependent_smem(weight_grad_kernel<G>, grid, kWgThreads, size_t(kWgSmem), st, w, dy_map, code_map);
     ++*launches;
     return launched(err, *launches);
@@ -270,9 +269,9 @@ extern "C" {
 int gaf_layer_workspace_bytes(int64_t T, int64_t width, int64_t V, int dtype, size_t *bytes_out) {
     if (!bytes_out || !in_range(T) || !in_range(width) || !in_range(V) || !is_dtype(dtype)) return GAF_ERR_ARG;
     // a weight gradient of at most width x width: the partial sums of split tokens are never more than this many tiles
-    const int64_t tiles = std::min(kWgMaxSplitItems, ceil_div(width, kWgM) * ceil_div(width, kWgN) *
+    const int64_t tiles = std::min(kWgMaxSplitItems, ceil_div(width, kWgPairM) * ceil_div(width, kWgN) *
                                                                ceil_div(ceil_div(T, kWgK) * (dtype == GAF_F32 ? 3 : 1), kWgChunkSteps));
-    size_t wg = kLayerScratchOffset + size_t(tiles) * kWgM * kWgN * 4 + 256;
+    size_t wg = kLayerScratchOffset + size_t(tiles) * kWgPairM * kWgN * 4 + 256;
     wg += size_t(dtype == GAF_F32 ? 3 : 1) * round_up(size_t(T), kWgK) * round_up(size_t(width), 8) * 2;
     const size_t a = embed_layout(T, width, V).end, b = norm_grad_bytes(width);
     *bytes_out = round_up(std::max(wg, std::max(a, b)), 256);
@@ -453,8 +452,8 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     DeviceInfo di;
     if (!device_info(&di)) return GAF_ERR_CUDA;
     // (a device with more SMs than the workspace was laid out for would split no further)
-    const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms, kWgMaxSplitItems));
-    if (p.steps * kWgK > kMaxRows) return GAF_ERR_TOO_LARGE;
+    const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms, 2 * kWgMaxSplitItems));
+    if (p.steps * kWgK > kMaxRows || p.tiles_m * p.tiles_n > INT32_MAX / kWgMaxSplitItems) return GAF_ERR_TOO_LARGE;
     const WgLayout l = weight_grad_layout(p, N, M, relaid);
     GAF_TRY(check_workspace(workspace, workspace_bytes, l.end));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -464,9 +463,9 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     w.scales = scales; w.base = base; w.dweight = dweight;
     w.partials = in_workspace<float>(workspace, l.partials);
     w.ctl = static_cast<Control *>(workspace);
-    w.T = T; w.N = N; w.M = M; w.blocks = blocks_of(M);
-    w.terms = dtype == GAF_F32 ? 3 : 1;
-    w.steps_per_term = p.steps_per_term; w.tiles_m = p.tiles_m; w.tiles_n = p.tiles_n; w.splits = p.splits; w.steps_per_split = p.steps_per_split;
+    w.T = int(T); w.N = N; w.M = M; w.blocks = int(blocks_of(M)); w.scale_bytes = T * blocks_of(M);
+    w.steps = int(p.steps); w.steps_per_term = int(std::max<int64_t>(1, p.steps_per_term)); w.steps_per_split = int(p.steps_per_split);
+    w.tiles_m = int(p.tiles_m); w.tiles = int(p.tiles_m * p.tiles_n); w.items = int(p.tiles_m * p.tiles_n * p.splits);
     w.spin_limit = test_wait_limit() ? test_wait_limit() : kTcSpinLimit;
     w.test_extra_arrival = test_withhold() & 1;
 

@@ -3,9 +3,14 @@
 //     dW[n, m] = base[n, m] + sum over tokens t of dy[t, n] * x[t, m]        x: the values of the codes
 //
 // 2 T N M operations on the 5th-generation tensor cores.  The tokens are the contraction axis, so both operands are
-// "MN-major": a row of either matrix is one step of the contraction.  The accumulator's 128 lanes are 128 columns m, the width of one
-// block of codes: a token has one scale per tile, and since the scale is a power of two, the values of the codes are exact in
+// "MN-major": a row of either matrix is one step of the contraction.  The accumulator's lanes are columns m; the 128 of a CTA are
+// one block of codes: a token has one scale per tile, and since the scale is a power of two, the values of the codes are exact in
 // bfloat16.  The codes are widened on their way through shared memory (8 bits cross the L2, not 16).
+//
+// Two CTAs on neighbouring SMs work on one tile of 256 m by 256 n (cta_group::2): each widens the codes of its own 128 m and
+// copies half of dy's columns, which the tensor cores of both read.  A tile of one CTA alone (128 x 256) would read 1.7 times as much
+// through the L2 and through shared memory, whose 128 bytes a clock are what bounds the kernel: per step of 64 tokens (512 clocks of
+// the tensor core) 24 KB are copied in, 8 KB read and 16 KB written by widening, 32 KB read by the MMAs.
 //
 // Accuracy.  A tensor core adds to its binary32 accumulator by cutting off, not by rounding; over many steps that pulls a sum
 // towards zero.  A chain therefore ends after kWgChunk tokens, and the chains are added, rounded to nearest, in registers of the epilogue's
@@ -13,9 +18,11 @@
 //
 // A CTA's warps (persistent; one CTA per SM):
 //   warps 0-7    epilogue: chains out of tensor memory into registers, the tile's result to global memory
-//   warps 8-11   widen codes: 16 at a time from the copied tile into the swizzled layout that the tensor core reads
-//   warp 12      tensor copies (TMA) of both matrices into a ring, bounded waits
-//   warp 13      issues the MMAs
+//   warps 8-15   widen codes: 16 at a time from the copied step into the swizzled layout that the tensor cores read
+//   warp 16      tensor copies (TMA) of both matrices into a ring
+//   warp 17      issues the MMAs (of the pair's first CTA)
+//   warp 18      copies the step's scale bytes (the aligned word that holds each)
+// Every wait is bounded.
 #pragma once
 
 #include "gaf_gram_tc.cuh"
@@ -23,13 +30,14 @@
 
 namespace gaf {
 
-constexpr int kWgM = 128, kWgN = 256, kWgK = 64;        // tile of dW, tokens per step
-constexpr int kWgStages = 4, kWgWide = 3;               // rings: copied steps, widened steps
+constexpr int kWgM = 128, kWgN = 256, kWgK = 64;        // a CTA's part of a tile of dW, tokens per step
+constexpr int kWgPairM = 2 * kWgM;                      // the pair's tile: 256 x 256
+constexpr int kWgStages = 5, kWgWide = 4;               // rings: copied steps, widened steps
 constexpr int kWgChunk = 256;                           // tokens per chain
 constexpr int kWgChunkSteps = kWgChunk / kWgK;
-constexpr int kWgDyBytes = kWgK * kWgN * 2, kWgCodeBytes = kWgK * kWgM, kWgWideBytes = kWgK * kWgM * 2;
+constexpr int kWgDyBytes = kWgK * (kWgN / 2) * 2, kWgCodeBytes = kWgK * kWgM, kWgWideBytes = kWgK * kWgM * 2;
 constexpr int kWgSmem = kWgStages * (kWgDyBytes + kWgCodeBytes) + kWgWide * kWgWideBytes + 1024;
-constexpr int kWgThreads = 512;
+constexpr int kWgThreads = 640;
 constexpr int kWgTmemCols = 512;
 
 struct WeightGradArgs {
@@ -38,19 +46,21 @@ struct WeightGradArgs {
     void *dweight;
     float *partials;            // [split][N][M], when the tokens are split
     Control *ctl;
-    int64_t T, N, M, blocks;    // blocks: scale bytes of a row
-    int terms;                  // 1; or 3: binary32 dy as the sum of three bfloat16 matrices, below one another
-    int64_t steps_per_term;     // ceil(T / kWgK)
-    int64_t tiles_m, tiles_n, splits, steps_per_split;      // (a multiple of kWgChunkSteps)
+    int64_t N, M, scale_bytes;
+    int T, blocks;              // blocks: scale bytes of a row
+    int steps, steps_per_term;  // steps of kWgK tokens; of each of the matrices that add up to dy
+    int tiles_m, items;         // items: tiles times splits
+    int tiles, steps_per_split; // (the latter a multiple of kWgChunkSteps)
     unsigned int spin_limit;
     int test_extra_arrival;     // test hook: the first barrier expects an arrival that never comes
 };
 
 struct WgShared {
     uint64_t full[kWgStages], empty[kWgStages];         // copied steps
-    uint64_t wide_full[kWgWide], wide_empty[kWgWide];   // widened steps
-    uint64_t acc_full[2], acc_empty[2];
+    uint64_t wide_full[kWgWide], wide_empty[kWgWide];   // widened steps (wide_full: of both CTAs, in the first one)
+    uint64_t acc_full[2], acc_empty[2];                 // chains (acc_empty: of both CTAs, in the first one)
     uint64_t drained;
+    uint32_t scale[kWgStages][kWgK];                    // the word that holds each token's scale byte
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -66,17 +76,49 @@ __device__ __forceinline__ uint64_t wg_desc(uint32_t smem_addr) {
     d |= (uint64_t)2 << 61;                             // 128-byte swizzle
     return d;
 }
-// bf16 x bf16 -> f32, both operands MN-major, M = 128, N = 256.
+// bf16 x bf16 -> f32, both operands MN-major, M = 256 over the pair, N = 256.
 constexpr uint32_t kWgInstrDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(kWgN >> 3) << 17) |
-                                  ((uint32_t)(kWgM >> 4) << 24);
+                                  ((uint32_t)(kWgPairM >> 4) << 24);
 
 __device__ __forceinline__ void wg_mma(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(kWgInstrDesc), "r"(accumulate)
         : "memory");
+}
+// All MMAs issued so far arrive, once complete, on the barrier at this place in both CTAs' shared memory.
+__device__ __forceinline__ void wg_commit_both(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(tc_smem_u32(bar)),
+                 "h"((unsigned short)3)
+                 : "memory");
+}
+__device__ __forceinline__ void wg_commit_own(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(tc_smem_u32(bar)) : "memory");
+}
+// The address, in the pair's first CTA, of what is at this place here; and an arrival there.
+__device__ __forceinline__ uint32_t wg_in_first(const void *p) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(tc_smem_u32(p)));
+    return r;
+}
+// 4-byte asynchronous copy that reads the first `src_bytes` (0..4) bytes and fills up with zeros.
+__device__ __forceinline__ void wg_copy4(uint32_t dst_smem, const void *src, uint32_t src_bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst_smem), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void wg_arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// 32 lanes x 16 columns of accumulators.
+__device__ __forceinline__ void wg_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
 // Four codes (bytes of w) as bfloat16 numbers 2^120 times too small: e4m3 and bfloat16 have their fields in the same order, so a
@@ -96,25 +138,55 @@ __device__ __forceinline__ unsigned int wg_power2(int e) {      // 2^e twice, e 
     const unsigned int p = (unsigned int)(e + 127) << 7;
     return p | (p << 16);
 }
+// 16 codes and their scale byte as bfloat16 numbers.
+__device__ __forceinline__ void wg_widen16(const uint4 &c, unsigned int scale, unsigned int (&out)[8]) {
+    const unsigned int in[4] = {c.x, c.y, c.z, c.w};
+    unsigned int nan = 0u;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) nan |= (in[q] & 0x7F7F7F7Fu) + 0x01010101u;
+    if (nan & 0x80808080u) {                                    // rare: some code is NaN
+        const float f = scale_of_byte(scale);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float2 x = value_pair((unsigned short)in[q]), y = value_pair((unsigned short)(in[q] >> 16));
+            out[2 * q] = pack_bf16x2(x.x * f, x.y * f);
+            out[2 * q + 1] = pack_bf16x2(y.x * f, y.y * f);
+        }
+        return;
+    }
+    // 2^(e + 120) in one multiplication where that is a number, else 2^120 first
+    const int e = (int)scale - 127;
+    const unsigned int f = e <= 7 ? wg_power2(e + 120) : wg_power2(120);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        wg_widen4(in[q], out[2 * q], out[2 * q + 1]);
+        out[2 * q] = wg_mul2(out[2 * q], f);
+        out[2 * q + 1] = wg_mul2(out[2 * q + 1], f);
+    }
+    if (e > 7) {
+        const unsigned int f2 = (scale << 7) | (scale << 23);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) out[q] = wg_mul2(out[q], f2);
+    }
+}
 
 // A work item: one tile of dW and one range of steps.
-struct WgItem { int64_t m0, n0, split, step0, step1; };
-__device__ __forceinline__ WgItem wg_item(const WeightGradArgs &a, int64_t item) {
+struct WgItem { int m0, n0, split, step0, step1; };             // m0: of this CTA's part
+__device__ __forceinline__ WgItem wg_item(const WeightGradArgs &a, int item, int rank) {
     WgItem w;
-    const int64_t tiles = a.tiles_m * a.tiles_n, steps = a.terms * a.steps_per_term;
-    w.split = item / tiles;
-    const int64_t tile = item - w.split * tiles;
-    w.n0 = (tile / a.tiles_m) * kWgN;
-    w.m0 = (tile % a.tiles_m) * kWgM;
+    w.split = item / a.tiles;
+    const int tile = item - w.split * a.tiles, tn = tile / a.tiles_m;
+    w.n0 = tn * kWgN;
+    w.m0 = (tile - tn * a.tiles_m) * kWgPairM + rank * kWgM;
     w.step0 = w.split * a.steps_per_split;
-    w.step1 = min(steps, w.step0 + a.steps_per_split);
+    w.step1 = min(a.steps, w.step0 + a.steps_per_split);
     return w;
 }
 
-// `dy_map`: {N, terms x rows of a term} of bfloat16, box {64, kWgK}, 128-byte swizzle; `code_map`: {M, T} of bytes, box {kWgM, kWgK}.  Both
+// `dy_map`: {N, rows of all terms} of bfloat16, box {64, kWgK}, 128-byte swizzle; `code_map`: {M, T} of bytes, box {kWgM, kWgK}.  Both
 // fill what lies outside with zeros.  G: type of dW (of the partial sums: float).
 template <typename G>
-__global__ void __launch_bounds__(kWgThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
 weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap dy_map,
                    const __grid_constant__ CUtensorMap code_map) {
     extern __shared__ unsigned char wg_dyn[];
@@ -123,224 +195,223 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     unsigned char *const dy_ring = smem, *const wide_ring = dy_ring + kWgStages * kWgDyBytes,
                          *const code_ring = wide_ring + kWgWide * kWgWideBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t n_items = a.tiles_m * a.tiles_n * a.splits;
+    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kWgStages; ++s) {
-            tc_mbar_init(&sh.full[s], 1 + (s == 0 && a.test_extra_arrival ? 1 : 0));
+            // the thread that copies, and the lanes that copy scales
+            tc_mbar_init(&sh.full[s], 33 + (s == 0 && a.test_extra_arrival ? 1 : 0));
             tc_mbar_init(&sh.empty[s], 1);
         }
         for (int s = 0; s < kWgWide; ++s) {
-            tc_mbar_init(&sh.wide_full[s], 128);
+            tc_mbar_init(&sh.wide_full[s], 16);          // 8 warps of either CTA
             tc_mbar_init(&sh.wide_empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             tc_mbar_init(&sh.acc_full[b], 1);
-            tc_mbar_init(&sh.acc_empty[b], 256);
+            tc_mbar_init(&sh.acc_empty[b], 16);
         }
         tc_mbar_init(&sh.drained, 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 13) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc_smem_u32(&sh.tmem_base)), "r"(kWgTmemCols)
+    if (warp == 17) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc_smem_u32(&sh.tmem_base)), "r"(kWgTmemCols)
                      : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before_sync();
     __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
     grid_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
 
-    // 4 x 128 threads with 128 registers each: 2 x 184 + 80 + 64 = 512
+    // 5 x 128 threads with 96 registers each: 2 x 168 + 2 x 48 + 48 = 480
     if (warp < 8) {
         // ------------------------------------------------------------ epilogue ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
-        int64_t chain = 0;
+        const uint32_t emptied[2] = {wg_in_first(&sh.acc_empty[0]), wg_in_first(&sh.acc_empty[1])};
+        uint32_t chain = 0;
         bool alive = true;
-        for (int64_t item = blockIdx.x; item < n_items && alive; item += gridDim.x) {
-            const WgItem w = wg_item(a, item);
+        for (int item = pair; item < a.items && alive; item += pairs) {
+            const WgItem w = wg_item(a, item, rank);
             float sum[128];
 #pragma unroll
             for (int j = 0; j < 128; ++j) sum[j] = 0.f;
-            for (int64_t step = w.step0; step < w.step1; step += kWgChunkSteps, ++chain) {
-                const int buf = (int)(chain & 1);
-                if (!tc_mbar_wait_warp(&sh.acc_full[buf], (uint32_t)((chain >> 1) & 1), &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+            for (int step = w.step0; step < w.step1; step += kWgChunkSteps, ++chain) {
+                const uint32_t buf = chain & 1u;
+                if (!tc_mbar_wait_warp(&sh.acc_full[buf], (chain >> 1) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                 tc_fence_after_sync();
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t r[32];
-                    tc_tmem_ld32(taddr + (uint32_t)(buf * kWgN + g * 32), r);
+                for (int g = 0; g < 8; ++g) {
+                    uint32_t r[16];
+                    wg_tmem_ld16(taddr + buf * kWgN + (uint32_t)(g * 16), r);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[g * 32 + j] += __uint_as_float(r[j]);
+                    for (int j = 0; j < 16; ++j) sum[g * 16 + j] += __uint_as_float(r[j]);
                 }
                 tc_fence_before_sync();
-                tc_mbar_arrive(&sh.acc_empty[buf]);
+                __syncwarp();
+                if (lane == 0) wg_arrive_remote(emptied[buf]);
             }
             if (!alive) break;
             const int64_t m = w.m0 + quarter * 32 + lane, n0 = w.n0 + half * 128;
             if (m < a.M) {
-                if (a.splits > 1) {
+                const int n = (int)min((int64_t)128, a.N - n0);
+                if (a.items > a.tiles) {
                     float *const out = a.partials + (w.split * a.N + n0) * a.M + m;
 #pragma unroll
                     for (int j = 0; j < 128; ++j)
-                        if (n0 + j < a.N) out[j * a.M] = sum[j];
+                        if (j < n) out[j * a.M] = sum[j];
                 } else {
                     const G *const base = static_cast<const G *>(a.base);
                     G *const out = static_cast<G *>(a.dweight) + n0 * a.M + m;
 #pragma unroll
                     for (int j = 0; j < 128; ++j)
-                        if (n0 + j < a.N) out[j * a.M] = from_float<G>(base ? sum[j] + to_float<G>(base[(n0 + j) * a.M + m]) : sum[j]);
+                        if (j < n) out[j * a.M] = from_float<G>(base ? sum[j] + to_float<G>(base[(n0 + j) * a.M + m]) : sum[j]);
                 }
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < 16) {
         // ------------------------------------------------------------ widening ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         const int tid = threadIdx.x - 256;
-        const int j = tid & 7, row0 = tid >> 3;          // 16 codes j of the rows row0, row0 + 16, ..
+        const int j = tid & 7, row = tid >> 3;           // 16 codes j of the rows row, row + 32
         // (half of the lanes write their two pieces in the other order: no two of eight lanes in the same banks)
-        const int swap = j >> 2;
-        uint32_t step_i = 0;                             // steps so far
+        const int swap = j >> 2, chunk = (2 * j) & 7;
+        const uint32_t line = (uint32_t)((j >> 2) * (kWgK * 128) + row * 128);
+        const uint32_t at0 = line + (((chunk + swap) ^ (row & 7)) << 4), at1 = line + (((chunk + 1 - swap) ^ (row & 7)) << 4);
+        int s = 0, o = 0;
+        uint32_t full_phase = 0, wide_phase = 1;         // (the first round finds every widened step's place free)
         bool alive = true;
-        for (int64_t item = blockIdx.x; item < n_items && alive; item += gridDim.x) {
-            const WgItem w = wg_item(a, item);
-            const unsigned char *const scale0 = a.scales + w.m0 / kCodeBlock;
-            // scale bytes of a step are fetched one step ahead
-            unsigned int next[4];
-            auto fetch = [&](int64_t step) {
-                const int64_t t0 = (step % a.steps_per_term) * kWgK + row0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) next[k] = step < w.step1 && t0 + 16 * k < a.T ? scale0[(t0 + 16 * k) * a.blocks] : 127u;
-            };
-            fetch(w.step0);
-            for (int64_t step = w.step0; step < w.step1; ++step, ++step_i) {
-                const int s = step_i % kWgStages, o = step_i % kWgWide;
-                unsigned int scale[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) scale[k] = next[k];
-                fetch(step + 1);
-                if (!tc_mbar_wait_warp(&sh.full[s], (step_i / kWgStages) & 1u, &sh.abort_flag, a.spin_limit) ||
-                    (step_i >= kWgWide &&
-                     !tc_mbar_wait_warp(&sh.wide_empty[o], (step_i / kWgWide - 1) & 1u, &sh.abort_flag, a.spin_limit))) { alive = false; break; }
-                const unsigned char *const codes = code_ring + s * kWgCodeBytes;
-                unsigned char *const wide = wide_ring + o * kWgWideBytes + (j >> 2) * (kWgK * 128);
-                uint4 c[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const uint4 *>(codes + (row0 + 16 * k) * kWgM + j * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned int in[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
-                    unsigned int out[8];
-                    unsigned int nan = 0u;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) nan |= (in[q] & 0x7F7F7F7Fu) + 0x01010101u;
-                    if (nan & 0x80808080u) {             // rare: some code is NaN
-                        const float f = scale_of_byte(scale[k]);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const float2 x = value_pair((unsigned short)in[q]), y = value_pair((unsigned short)(in[q] >> 16));
-                            out[2 * q] = pack_bf16x2(x.x * f, x.y * f);
-                            out[2 * q + 1] = pack_bf16x2(y.x * f, y.y * f);
-                        }
-                    } else {
-                        // 2^(e + 120) in one multiplication where that is a number, else 2^120 first
-                        const int e = (int)scale[k] - 127;
-                        const unsigned int f = e <= 7 ? wg_power2(max(e + 120, -126)) : wg_power2(120);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            wg_widen4(in[q], out[2 * q], out[2 * q + 1]);
-                            out[2 * q] = wg_mul2(out[2 * q], f);
-                            out[2 * q + 1] = wg_mul2(out[2 * q + 1], f);
-                        }
-                        if (e > 7) {
-                            const unsigned int f2 = (scale[k] << 7) | (scale[k] << 23);
-#pragma unroll
-                            for (int q = 0; q < 8; ++q) out[q] = wg_mul2(out[q], f2);
-                        }
-                    }
-                    const int row = row0 + 16 * k;
-                    unsigned char *const line = wide + row * 128;
-                    const int chunk = (2 * j) & 7;
-                    const uint4 p0 = make_uint4(out[0], out[1], out[2], out[3]), p1 = make_uint4(out[4], out[5], out[6], out[7]);
-                    *reinterpret_cast<uint4 *>(line + (((chunk + swap) ^ (row & 7)) << 4)) = swap ? p1 : p0;
-                    *reinterpret_cast<uint4 *>(line + (((chunk + 1 - swap) ^ (row & 7)) << 4)) = swap ? p0 : p1;
-                }
-                tc_fence_async_smem();                   // the tensor core reads through the asynchronous proxy
-                tc_mbar_arrive(&sh.wide_full[o]);
+        for (int item = pair; item < a.items && alive; item += pairs) {
+            const WgItem w = wg_item(a, item, rank);
+            // (64 tokens further on, a scale byte lies at the same place of its word)
+            const int shift0 = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8, shift1 = (((row + 32) * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
+            for (int step = w.step0; step < w.step1; ++step) {
+                if (!tc_mbar_wait_warp(&sh.full[s], full_phase, &sh.abort_flag, a.spin_limit) ||
+                    !tc_mbar_wait_warp(&sh.wide_empty[o], wide_phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                const unsigned char *const codes = code_ring + s * kWgCodeBytes + row * kWgM + j * 16;
+                unsigned char *const wide = wide_ring + o * kWgWideBytes;
+                const uint4 c0 = *reinterpret_cast<const uint4 *>(codes), c1 = *reinterpret_cast<const uint4 *>(codes + 32 * kWgM);
+                const unsigned int e0 = (sh.scale[s][row] >> shift0) & 0xFFu, e1 = (sh.scale[s][row + 32] >> shift1) & 0xFFu;
+                unsigned int v[8];
+                wg_widen16(c0, e0, v);
+                const uint4 p0 = make_uint4(v[0], v[1], v[2], v[3]), p1 = make_uint4(v[4], v[5], v[6], v[7]);
+                *reinterpret_cast<uint4 *>(wide + at0) = swap ? p1 : p0;
+                *reinterpret_cast<uint4 *>(wide + at1) = swap ? p0 : p1;
+                wg_widen16(c1, e1, v);
+                const uint4 q0 = make_uint4(v[0], v[1], v[2], v[3]), q1 = make_uint4(v[4], v[5], v[6], v[7]);
+                *reinterpret_cast<uint4 *>(wide + at0 + 32 * 128) = swap ? q1 : q0;
+                *reinterpret_cast<uint4 *>(wide + at1 + 32 * 128) = swap ? q0 : q1;
+                tc_fence_async_smem();                   // the tensor cores read through the asynchronous proxy
+                __syncwarp();
+                // (this CTA's part of dy has landed too: it completes the same barrier as the codes)
+                if (lane == 0) wg_arrive_remote(wg_in_first(&sh.wide_full[o]));
+                if (++s == kWgStages) { s = 0; full_phase ^= 1u; }
+                if (++o == kWgWide) { o = 0; wide_phase ^= 1u; }
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == 16) {
             // -------------------------------------------------------- copies ----
             if (lane == 0) {
-                uint32_t step_i = 0;
+                int s = 0;
+                uint32_t phase = 1, issued = 0;          // (every place is free at first)
                 bool alive = true;
-                for (int64_t item = blockIdx.x; item < n_items && alive; item += gridDim.x) {
-                    const WgItem w = wg_item(a, item);
-                    for (int64_t step = w.step0; step < w.step1; ++step, ++step_i) {
-                        const int s = step_i % kWgStages;
-                        if (step_i >= kWgStages &&
-                            !tc_mbar_wait(&sh.empty[s], (step_i / kWgStages - 1) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        const int32_t t0 = (int32_t)((step % a.steps_per_term) * kWgK), y0 = (int32_t)(step * kWgK);
+                for (int item = pair; item < a.items && alive; item += pairs) {
+                    const WgItem w = wg_item(a, item, rank);
+                    const int n0 = w.n0 + rank * (kWgN / 2);
+                    int t_step = w.step0 % a.steps_per_term;
+                    for (int step = w.step0; step < w.step1; ++step, ++issued) {
+                        if (!tc_mbar_wait(&sh.empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                         tc_mbar_arrive_expect_tx(&sh.full[s], kWgDyBytes + kWgCodeBytes);
-                        tc_tma_load_2d(tc_smem_u32(code_ring + s * kWgCodeBytes), &code_map, (int32_t)w.m0, t0, &sh.full[s]);
+                        tc_tma_load_2d(tc_smem_u32(code_ring + s * kWgCodeBytes), &code_map, w.m0, t_step * kWgK, &sh.full[s]);
 #pragma unroll
-                        for (int k = 0; k < kWgN / 64; ++k)
-                            tc_tma_load_2d(tc_smem_u32(dy_ring + s * kWgDyBytes + k * (kWgK * 128)), &dy_map, (int32_t)(w.n0 + 64 * k), y0, &sh.full[s]);
+                        for (int k = 0; k < kWgN / 128; ++k)
+                            tc_tma_load_2d(tc_smem_u32(dy_ring + s * kWgDyBytes + k * (kWgK * 128)), &dy_map, n0 + 64 * k, step * kWgK, &sh.full[s]);
+                        if (++t_step == a.steps_per_term) t_step = 0;
+                        if (++s == kWgStages) { s = 0; phase ^= 1u; }
                     }
                 }
                 // what is in flight lands before the CTA ends, also after a wait gave up
-                for (uint32_t i = step_i > kWgStages ? step_i - kWgStages : 0; i < step_i; ++i)
+                for (uint32_t i = issued > kWgStages ? issued - kWgStages : 0; i < issued; ++i)
                     for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
                         if (tc_mbar_try(&sh.full[i % kWgStages], (i / kWgStages) & 1u, 2000u)) break;
             }
             __syncwarp();
-        } else if (warp == 13) {
+        } else if (warp == 17) {
             // -------------------------------------------------------- MMA -------
-            if (lane == 0) {
-                uint32_t step_i = 0;
-                int64_t chain = 0;
+            if (rank == 0 && lane == 0) {
+                int s = 0, o = 0;
+                uint32_t phase = 0, chain = 0;
                 bool alive = true;
-                for (int64_t item = blockIdx.x; item < n_items && alive; item += gridDim.x) {
-                    const WgItem w = wg_item(a, item);
-                    for (int64_t step = w.step0; step < w.step1; ++step, ++step_i) {
-                        const int s = step_i % kWgStages, o = step_i % kWgWide;
-                        const int in_chain = (int)((step - w.step0) % kWgChunkSteps), buf = (int)(chain & 1);
-                        if (in_chain == 0 && chain >= 2 &&
-                            !tc_mbar_wait(&sh.acc_empty[buf], (uint32_t)((chain / 2 - 1) & 1), &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        if (!tc_mbar_wait(&sh.full[s], (step_i / kWgStages) & 1u, &sh.abort_flag, a.spin_limit) ||
-                            !tc_mbar_wait(&sh.wide_full[o], (step_i / kWgWide) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                for (int item = pair; item < a.items && alive; item += pairs) {
+                    const WgItem w = wg_item(a, item, rank);
+                    int in_chain = 0;
+                    for (int step = w.step0; step < w.step1; ++step) {
+                        const uint32_t buf = chain & 1u;
+                        if (in_chain == 0 && !tc_mbar_wait(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!tc_mbar_wait(&sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                         tc_fence_after_sync();
                         const uint64_t da = wg_desc(tc_smem_u32(wide_ring + o * kWgWideBytes)), db = wg_desc(tc_smem_u32(dy_ring + s * kWgDyBytes));
 #pragma unroll
                         for (int k = 0; k < kWgK / 16; ++k)       // 16 tokens = 2048 bytes on
-                            wg_mma(tmem + (uint32_t)(buf * kWgN), da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), in_chain || k ? 1u : 0u);
-                        tc_commit(&sh.empty[s]);
-                        tc_commit(&sh.wide_empty[o]);
-                        if (in_chain == kWgChunkSteps - 1 || step + 1 == w.step1) {
-                            tc_commit(&sh.acc_full[buf]);
+                            wg_mma(tmem + buf * kWgN, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), in_chain || k ? 1u : 0u);
+                        wg_commit_both(&sh.empty[s]);
+                        wg_commit_both(&sh.wide_empty[o]);
+                        if (++in_chain == kWgChunkSteps || step + 1 == w.step1) {
+                            wg_commit_both(&sh.acc_full[buf]);
                             ++chain;
+                            in_chain = 0;
                         }
+                        if (++s == kWgStages) s = 0;
+                        if (++o == kWgWide) { o = 0; phase ^= 1u; }
                     }
                 }
-                // tensor memory is not freed under MMAs in flight
-                tc_commit(&sh.drained);
+                // tensor memory is not freed, and no shared memory left, under MMAs in flight
+                wg_commit_own(&sh.drained);
                 for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
                     if (tc_mbar_try(&sh.drained, 0u, 2000u)) break;
             }
             __syncwarp();
+        } else if (warp == 18) {
+            // -------------------------------------------------------- scales ----
+            int s = 0;
+            uint32_t phase = 1;
+            bool alive = true;
+            for (int item = pair; item < a.items && alive; item += pairs) {
+                const WgItem w = wg_item(a, item, rank);
+                const int block = w.m0 / kCodeBlock;
+                int t_step = w.step0 % a.steps_per_term;
+                for (int step = w.step0; step < w.step1; ++step) {
+                    if (!tc_mbar_wait_warp(&sh.empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int t = t_step * kWgK + lane + 32 * k;
+                        const int64_t byte = (int64_t)t * a.blocks + block, word = byte & ~int64_t(3);
+                        const bool in = t < a.T && block < a.blocks;
+                        wg_copy4(tc_smem_u32(&sh.scale[s][lane + 32 * k]), in ? a.scales + word : a.scales,
+                                           in ? (uint32_t)min((int64_t)4, a.scale_bytes - word) : 0u);
+                    }
+                    tc_cp_async_arrive(&sh.full[s]);
+                    if (++t_step == a.steps_per_term) t_step = 0;
+                    if (++s == kWgStages) { s = 0; phase ^= 1u; }
+                }
+            }
+            tc_cp_async_wait_all();
         }
     }
     tc_fence_before_sync();
     __syncthreads();
+    // neither CTA leaves, or frees its tensor memory, while the other's MMAs or arrivals can still reach it
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     tc_fence_after_sync();
-    if (warp == 13) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kWgTmemCols) : "memory");
+    if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kWgTmemCols) : "memory");
     if (sh.abort_flag && threadIdx.x == 0) atomicOr(&a.ctl->status, kStatusTimeoutBit);
 }
 
