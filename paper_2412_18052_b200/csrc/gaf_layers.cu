@@ -493,7 +493,7 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
         }
         if (!matrix_map(&dy_map, y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, N, y_rows, y_pitch, 64, kWgK, CU_TENSOR_MAP_SWIZZLE_128B) ||
             !matrix_map(&code_map, codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, M, T, T > 1 ? codes_stride : int64_t(round_up(size_t(M), 16)),
-                        kWgM, kWgK, CU_TENSOR_MAP_SWIZZLE_NONE))
+                        kWgM, kWgK, CU_TENSOR_MAP_SWIZZLE_128B))
             return GAF_ERR_CUDA;
     }
     GAF_TRY(grad_dtype == GAF_F32 ? launch_weight_grad_tiles<float>(w, dy_map, code_map, di, st, &launches)

@@ -19,10 +19,16 @@
 // A CTA's warps (persistent; one CTA per SM):
 //   warps 0-7    epilogue: chains out of tensor memory into registers, the tile's result to global memory
 //   warps 8-15   widen codes: 16 at a time from the copied step into the swizzled layout that the tensor cores read
-//   warp 16      tensor copies (TMA) of both matrices into a ring
-//   warp 17      issues the MMAs (of the pair's first CTA)
-//   warp 18      copies the step's scale bytes (the aligned word that holds each)
-// Every wait is bounded.
+//   warp 16      tensor copies (TMA) of dy
+//   warp 17      issues the MMAs (in the pair's first CTA; in the second it tells the first what is ready)
+//   warp 18      tensor copies of the codes
+//   warp 19      copies of their scale bytes (the aligned word that holds each)
+// An arrival on a barrier costs tens of clocks, one after the other: wherever a step is handed on, one lane of a warp arrives.  And it
+// waits for the loads that its thread has in flight: the widening warps have none (scale bytes that they fetched a step ahead themselves
+// cost 0.7 us a step), the scales come by asynchronous copies.
+// Three rings: codes, whose places are free again as soon as they are in registers, widened codes, and dy, both free when the MMAs have
+// read them.  (One ring for codes and dy kept a step's codes until its MMAs were done: copy, widening and MMAs together
+// take 4000 clocks, and five steps in flight left 800 a step.)  Every wait is bounded.
 #pragma once
 
 #include "gaf_gram_tc.cuh"
@@ -30,14 +36,17 @@
 
 namespace gaf {
 
-constexpr int kWgM = 128, kWgN = 256, kWgK = 64;        // a CTA's part of a tile of dW, tokens per step
+constexpr int kWgM = 128, kWgN = 256, kWgK = 128;        // a CTA's part of a tile of dW, tokens per step
 constexpr int kWgPairM = 2 * kWgM;                      // the pair's tile: 256 x 256
-constexpr int kWgStages = 5, kWgWide = 4;               // rings: copied steps, widened steps
-constexpr int kWgChunk = 256;                           // tokens per chain
+constexpr int kWgRing = 3, kWgCodeRing = 2;             // steps in the rings: dy and widened codes; codes
+constexpr int kWgChunk = 512;                           // tokens per chain
 constexpr int kWgChunkSteps = kWgChunk / kWgK;
 constexpr int kWgDyBytes = kWgK * (kWgN / 2) * 2, kWgCodeBytes = kWgK * kWgM, kWgWideBytes = kWgK * kWgM * 2;
-constexpr int kWgSmem = kWgStages * (kWgDyBytes + kWgCodeBytes) + kWgWide * kWgWideBytes + 1024;
+constexpr int kWgSmem = kWgRing * (kWgDyBytes + kWgWideBytes) + kWgCodeRing * kWgCodeBytes + 1024;
+constexpr int kWgGroups = 1;                            // groups of the widening warps, which take steps in turn
+constexpr uint32_t kWgScalesAhead = 1;                  // steps whose scales are in flight (less than the ring holds)
 constexpr int kWgThreads = 640;
+constexpr int kWgNapEpilogue = 400, kWgNapWiden = 0, kWgNapCopy = 100, kWgNapMma = 0;
 constexpr int kWgTmemCols = 512;
 
 struct WeightGradArgs {
@@ -56,11 +65,12 @@ struct WeightGradArgs {
 };
 
 struct WgShared {
-    uint64_t full[kWgStages], empty[kWgStages];         // copied steps
-    uint64_t wide_full[kWgWide], wide_empty[kWgWide];   // widened steps (wide_full: of both CTAs, in the first one)
+    uint64_t code_full[kWgCodeRing], code_empty[kWgCodeRing];
+    uint64_t dy_full[kWgRing], wide_full[kWgRing], done[kWgRing];  // done: the MMAs have read dy and the widened codes
+    uint64_t other[kWgRing];                            // the second CTA's steps that are ready for the MMAs, in the first one
     uint64_t acc_full[2], acc_empty[2];                 // chains (acc_empty: of both CTAs, in the first one)
     uint64_t drained;
-    uint32_t scale[kWgStages][kWgK];                    // the word that holds each token's scale byte
+    uint32_t scale[kWgCodeRing][kWgK];                  // the word that holds each token's scale byte
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -107,17 +117,56 @@ __device__ __forceinline__ uint32_t wg_in_first(const void *p) {
 __device__ __forceinline__ void wg_copy4(uint32_t dst_smem, const void *src, uint32_t src_bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst_smem), "l"(src), "r"(src_bytes) : "memory");
 }
-__device__ __forceinline__ void wg_arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// One lane of the warp, always the same.
+__device__ __forceinline__ bool wg_elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
-// 32 lanes x 16 columns of accumulators.
-__device__ __forceinline__ void wg_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+// Bounded waits.  An attempt returns within tens of clocks whether or not the phase is complete, and a warp that polls takes issue
+// slots from the widening warps: who can afford it sleeps between attempts (`nap` nanoseconds).  A warp polls, and arrives, without
+// branching on the lane: after `if (lane == 0) ..` it went on in two parts, and executed everything twice (1223 -> 868 us at 16384 x 4096 x 4096).
+template <int nap>
+__device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
+    for (unsigned int spin = 0; spin < limit; ++spin) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(tc_smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (nap > 0) __nanosleep(nap);
+        if ((spin & 15u) == 15u && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    return false;
+}
+template <int nap>
+__device__ __forceinline__ bool wg_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
+    return __all_sync(0xFFFFFFFFu, wg_wait<nap>(bar, parity, abort_flag, limit)) != 0;
+}
+// One lane's arrival for its whole warp, here or at the same place in the pair's first CTA.
+__device__ __forceinline__ void wg_arrive_warp(uint64_t *bar) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(tc_smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void wg_arrive_warp_in_first(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}" ::"r"(wg_in_first(bar)) : "memory");
+}
+// 32 lanes x 8 columns of accumulators.
+__device__ __forceinline__ void wg_tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
@@ -134,39 +183,35 @@ __device__ __forceinline__ unsigned int wg_mul2(unsigned int a, unsigned int b) 
     const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
     return *reinterpret_cast<const unsigned int *>(&r);
 }
-__device__ __forceinline__ unsigned int wg_power2(int e) {      // 2^e twice, e in -126..127
-    const unsigned int p = (unsigned int)(e + 127) << 7;
-    return p | (p << 16);
+// Not zero if one of 16 codes is NaN, or the scale above 2^7 (then the factor of wg_widen16 is no number).
+__device__ __forceinline__ unsigned int wg_unusual(const uint4 &c, unsigned int scale) {
+    const unsigned int n = ((c.x & 0x7F7F7F7Fu) + 0x01010101u) | ((c.y & 0x7F7F7F7Fu) + 0x01010101u) | ((c.z & 0x7F7F7F7Fu) + 0x01010101u) |
+                           ((c.w & 0x7F7F7F7Fu) + 0x01010101u);
+    return (n & 0x80808080u) | (unsigned int)(scale > 134u);
 }
-// 16 codes and their scale byte as bfloat16 numbers.
+// 16 codes and their scale byte as bfloat16 numbers: one multiplication by 2^(e + 120).
 __device__ __forceinline__ void wg_widen16(const uint4 &c, unsigned int scale, unsigned int (&out)[8]) {
-    const unsigned int in[4] = {c.x, c.y, c.z, c.w};
-    unsigned int nan = 0u;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) nan |= (in[q] & 0x7F7F7F7Fu) + 0x01010101u;
-    if (nan & 0x80808080u) {                                    // rare: some code is NaN
-        const float f = scale_of_byte(scale);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float2 x = value_pair((unsigned short)in[q]), y = value_pair((unsigned short)(in[q] >> 16));
-            out[2 * q] = pack_bf16x2(x.x * f, x.y * f);
-            out[2 * q + 1] = pack_bf16x2(y.x * f, y.y * f);
-        }
-        return;
-    }
-    // 2^(e + 120) in one multiplication where that is a number, else 2^120 first
-    const int e = (int)scale - 127;
-    const unsigned int f = e <= 7 ? wg_power2(e + 120) : wg_power2(120);
+    const unsigned int in[4] = {c.x, c.y, c.z, c.w}, f = (scale + 120u) * 0x00800080u;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         wg_widen4(in[q], out[2 * q], out[2 * q + 1]);
         out[2 * q] = wg_mul2(out[2 * q], f);
         out[2 * q + 1] = wg_mul2(out[2 * q + 1], f);
     }
-    if (e > 7) {
-        const unsigned int f2 = (scale << 7) | (scale << 23);
+}
+// The same for any codes and scale: by 2^127 first where 2^(e + 120) is no number, and codes of NaN become NaN.  (A value beyond
+// bfloat16's range becomes infinite, which no code that was packed does.)
+__device__ __forceinline__ void wg_widen16_any(const uint4 &c, unsigned int scale, unsigned int (&out)[8]) {
+    const unsigned int in[4] = {c.x, c.y, c.z, c.w};
+    const unsigned int f1 = min(scale + 120u, 254u) * 0x00800080u, f2 = scale > 134u ? (scale - 7u) * 0x00800080u : 0x3F803F80u;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) out[q] = wg_mul2(out[q], f2);
+    for (int q = 0; q < 4; ++q) {
+        wg_widen4(in[q], out[2 * q], out[2 * q + 1]);
+#pragma unroll
+        for (int h = 2 * q; h < 2 * q + 2; ++h) {
+            const unsigned int nan = __vcmpeq2(out[h] & 0x7FFF7FFFu, 0x07F007F0u);
+            out[h] = wg_mul2(wg_mul2(out[h], f1), f2) | (nan & 0x7FFF7FFFu);
+        }
     }
 }
 
@@ -183,8 +228,8 @@ __device__ __forceinline__ WgItem wg_item(const WeightGradArgs &a, int item, int
     return w;
 }
 
-// `dy_map`: {N, rows of all terms} of bfloat16, box {64, kWgK}, 128-byte swizzle; `code_map`: {M, T} of bytes, box {kWgM, kWgK}.  Both
-// fill what lies outside with zeros.  G: type of dW (of the partial sums: float).
+// `dy_map`: {N, rows of all terms} of bfloat16, box {64, kWgK}, 128-byte swizzle; `code_map`: {M, T} of bytes, box {kWgM, kWgK}, the
+// same swizzle.  Both fill what lies outside with zeros.  G: type of dW (of the partial sums: float).
 template <typename G>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgThreads, 1)
 weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_constant__ CUtensorMap dy_map,
@@ -192,20 +237,22 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     extern __shared__ unsigned char wg_dyn[];
     __shared__ WgShared sh;
     unsigned char *const smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(wg_dyn) + 1023) & ~uintptr_t(1023));
-    unsigned char *const dy_ring = smem, *const wide_ring = dy_ring + kWgStages * kWgDyBytes,
-                         *const code_ring = wide_ring + kWgWide * kWgWideBytes;
+    unsigned char *const dy_ring = smem, *const wide_ring = dy_ring + kWgRing * kWgDyBytes,
+                         *const code_ring = wide_ring + kWgRing * kWgWideBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kWgStages; ++s) {
-            // the thread that copies, and the lanes that copy scales
-            tc_mbar_init(&sh.full[s], 33 + (s == 0 && a.test_extra_arrival ? 1 : 0));
-            tc_mbar_init(&sh.empty[s], 1);
+        for (int s = 0; s < kWgCodeRing; ++s) {
+            // codes, scales
+            tc_mbar_init(&sh.code_full[s], 2 + (s == 0 && a.test_extra_arrival ? 1 : 0));
+            tc_mbar_init(&sh.code_empty[s], 8 / kWgGroups);
         }
-        for (int s = 0; s < kWgWide; ++s) {
-            tc_mbar_init(&sh.wide_full[s], 16);          // 8 warps of either CTA
-            tc_mbar_init(&sh.wide_empty[s], 1);
+        for (int s = 0; s < kWgRing; ++s) {
+            tc_mbar_init(&sh.dy_full[s], 1);
+            tc_mbar_init(&sh.wide_full[s], 8 / kWgGroups);   // a group's warps
+            tc_mbar_init(&sh.done[s], 1);
+            tc_mbar_init(&sh.other[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             tc_mbar_init(&sh.acc_full[b], 1);
@@ -228,13 +275,13 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     grid_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
 
-    // 5 x 128 threads with 96 registers each: 2 x 168 + 2 x 48 + 48 = 480
+    // 5 x 128 threads with 96 registers each: 2 x 160 + 2 x 56 + 48 = 480 (nothing spills: what a thread stores to local memory, its
+    // fence for the tensor cores would wait for)
     if (warp < 8) {
         // ------------------------------------------------------------ epilogue ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
-        const uint32_t emptied[2] = {wg_in_first(&sh.acc_empty[0]), wg_in_first(&sh.acc_empty[1])};
         uint32_t chain = 0;
         bool alive = true;
         for (int item = pair; item < a.items && alive; item += pairs) {
@@ -244,18 +291,18 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             for (int j = 0; j < 128; ++j) sum[j] = 0.f;
             for (int step = w.step0; step < w.step1; step += kWgChunkSteps, ++chain) {
                 const uint32_t buf = chain & 1u;
-                if (!tc_mbar_wait_warp(&sh.acc_full[buf], (chain >> 1) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                if (!wg_wait_warp<kWgNapEpilogue>(&sh.acc_full[buf], (chain >> 1) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                 tc_fence_after_sync();
 #pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    uint32_t r[16];
-                    wg_tmem_ld16(taddr + buf * kWgN + (uint32_t)(g * 16), r);
+                for (int g = 0; g < 16; ++g) {
+                    uint32_t r[8];
+                    wg_tmem_ld8(taddr + buf * kWgN + (uint32_t)(g * 8), r);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sum[g * 16 + j] += __uint_as_float(r[j]);
+                    for (int j = 0; j < 8; ++j) sum[g * 8 + j] += __uint_as_float(r[j]);
                 }
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) wg_arrive_remote(emptied[buf]);
+                wg_arrive_warp_in_first(&sh.acc_empty[buf]);
             }
             if (!alive) break;
             const int64_t m = w.m0 + quarter * 32 + lane, n0 = w.n0 + half * 128;
@@ -277,48 +324,71 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         }
     } else if (warp < 16) {
         // ------------------------------------------------------------ widening ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        const int tid = threadIdx.x - 256;
-        const int j = tid & 7, row = tid >> 3;           // 16 codes j of the rows row, row + 32
-        // (half of the lanes write their two pieces in the other order: no two of eight lanes in the same banks)
-        const int swap = j >> 2, chunk = (2 * j) & 7;
-        const uint32_t line = (uint32_t)((j >> 2) * (kWgK * 128) + row * 128);
-        const uint32_t at0 = line + (((chunk + swap) ^ (row & 7)) << 4), at1 = line + (((chunk + 1 - swap) ^ (row & 7)) << 4);
-        int s = 0, o = 0;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        constexpr int kRows = 8 * (8 / kWgGroups), kUnits = kWgK / kRows;       // rows of a group at a time
+        const int group = (warp - 8) / (8 / kWgGroups);
+        // A unit is 16 codes of a row.  Four lanes take the four units of half a row (64 codes, one swizzle atom of the widened step), the four
+        // lanes next to them those of the row whose number differs by 5: then neither the codes (swizzled by the copy) nor what is written
+        // meets another lane's banks.  A warp takes 8 rows at a time.
+        const int j = lane & 3, pair_of = lane >> 3, row = ((pair_of & 3) ^ ((lane & 4) ? 5 : 0)) + (warp - 8) % (8 / kWgGroups) * 8;
+        const uint32_t code_at = (uint32_t)(row * kWgM + ((j ^ (row & 7)) << 4));                   // first half of the row; the second: ^ 64
+        const uint32_t at0 = (uint32_t)(row * 128 + ((2 * j) ^ (row & 7)) * 16), at1 = (uint32_t)(row * 128 + ((2 * j + 1) ^ (row & 7)) * 16);
+        int s = group, o = group, skip = group;          // skip: steps of the other groups before the next one of this
         uint32_t full_phase = 0, wide_phase = 1;         // (the first round finds every widened step's place free)
         bool alive = true;
         for (int item = pair; item < a.items && alive; item += pairs) {
             const WgItem w = wg_item(a, item, rank);
-            // (64 tokens further on, a scale byte lies at the same place of its word)
-            const int shift0 = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8, shift1 = (((row + 32) * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
-            for (int step = w.step0; step < w.step1; ++step) {
-                if (!tc_mbar_wait_warp(&sh.full[s], full_phase, &sh.abort_flag, a.spin_limit) ||
-                    !tc_mbar_wait_warp(&sh.wide_empty[o], wide_phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                const unsigned char *const codes = code_ring + s * kWgCodeBytes + row * kWgM + j * 16;
+            // (a multiple of 4 tokens further on, a scale byte lies at the same place of its word)
+            const int shift = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
+            int step = w.step0 + skip;
+            for (; step < w.step1; step += kWgGroups) {
+                // (two lanes poll the codes' barrier and that of the place they go to)
+                if (!wg_wait_warp<kWgNapWiden>(lane == 0 ? &sh.code_full[s] : &sh.done[o], lane == 0 ? full_phase : wide_phase, &sh.abort_flag,
+                                               a.spin_limit)) { alive = false; break; }
+                const unsigned char *const codes = code_ring + s * kWgCodeBytes;
                 unsigned char *const wide = wide_ring + o * kWgWideBytes;
-                const uint4 c0 = *reinterpret_cast<const uint4 *>(codes), c1 = *reinterpret_cast<const uint4 *>(codes + 32 * kWgM);
-                const unsigned int e0 = (sh.scale[s][row] >> shift0) & 0xFFu, e1 = (sh.scale[s][row + 32] >> shift1) & 0xFFu;
-                unsigned int v[8];
-                wg_widen16(c0, e0, v);
-                const uint4 p0 = make_uint4(v[0], v[1], v[2], v[3]), p1 = make_uint4(v[4], v[5], v[6], v[7]);
-                *reinterpret_cast<uint4 *>(wide + at0) = swap ? p1 : p0;
-                *reinterpret_cast<uint4 *>(wide + at1) = swap ? p0 : p1;
-                wg_widen16(c1, e1, v);
-                const uint4 q0 = make_uint4(v[0], v[1], v[2], v[3]), q1 = make_uint4(v[4], v[5], v[6], v[7]);
-                *reinterpret_cast<uint4 *>(wide + at0 + 32 * 128) = swap ? q1 : q0;
-                *reinterpret_cast<uint4 *>(wide + at1 + 32 * 128) = swap ? q0 : q1;
-                tc_fence_async_smem();                   // the tensor cores read through the asynchronous proxy
+                uint4 c[2 * kUnits];
+                unsigned int e[kUnits], unusual = 0u;
+#pragma unroll
+                for (int k = 0; k < kUnits; ++k) {
+                    c[2 * k] = *reinterpret_cast<const uint4 *>(codes + code_at + k * kRows * kWgM);
+                    c[2 * k + 1] = *reinterpret_cast<const uint4 *>(codes + (code_at ^ 64u) + k * kRows * kWgM);
+                    e[k] = (sh.scale[s][row + k * kRows] >> shift) & 0xFFu;
+                }
                 __syncwarp();
-                // (this CTA's part of dy has landed too: it completes the same barrier as the codes)
-                if (lane == 0) wg_arrive_remote(wg_in_first(&sh.wide_full[o]));
-                if (++s == kWgStages) { s = 0; full_phase ^= 1u; }
-                if (++o == kWgWide) { o = 0; wide_phase ^= 1u; }
+                wg_arrive_warp(&sh.code_empty[s]);
+#pragma unroll
+                for (int k = 0; k < 2 * kUnits; ++k) unusual |= wg_unusual(c[k], e[k >> 1]);
+                if (unusual == 0u) {
+#pragma unroll
+                    for (int k = 0; k < 2 * kUnits; ++k) {
+                        unsigned int v[8];
+                        wg_widen16(c[k], e[k >> 1], v);
+                        unsigned char *const to = wide + (k & 1) * (kWgK * 128) + (k >> 1) * kRows * 128;
+                        *reinterpret_cast<uint4 *>(to + at0) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4 *>(to + at1) = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2 * kUnits; ++k) {
+                        unsigned int v[8];
+                        wg_widen16_any(c[k], e[k >> 1], v);
+                        unsigned char *const to = wide + (k & 1) * (kWgK * 128) + (k >> 1) * kRows * 128;
+                        *reinterpret_cast<uint4 *>(to + at0) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4 *>(to + at1) = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+                __syncwarp();
+                wg_arrive_warp(&sh.wide_full[o]);
+                if ((s += kWgGroups) >= kWgCodeRing) { s -= kWgCodeRing; full_phase ^= 1u; }
+                if ((o += kWgGroups) >= kWgRing) { o -= kWgRing; wide_phase ^= 1u; }
             }
+            skip = step - w.step1;
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (warp == 16) {
-            // -------------------------------------------------------- copies ----
+            // ------------------------------------------------- copies of dy ----
             if (lane == 0) {
                 int s = 0;
                 uint32_t phase = 1, issued = 0;          // (every place is free at first)
@@ -326,84 +396,143 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 for (int item = pair; item < a.items && alive; item += pairs) {
                     const WgItem w = wg_item(a, item, rank);
                     const int n0 = w.n0 + rank * (kWgN / 2);
-                    int t_step = w.step0 % a.steps_per_term;
                     for (int step = w.step0; step < w.step1; ++step, ++issued) {
-                        if (!tc_mbar_wait(&sh.empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        tc_mbar_arrive_expect_tx(&sh.full[s], kWgDyBytes + kWgCodeBytes);
-                        tc_tma_load_2d(tc_smem_u32(code_ring + s * kWgCodeBytes), &code_map, w.m0, t_step * kWgK, &sh.full[s]);
+                        if (!wg_wait<kWgNapCopy>(&sh.done[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        tc_mbar_arrive_expect_tx(&sh.dy_full[s], kWgDyBytes);
 #pragma unroll
                         for (int k = 0; k < kWgN / 128; ++k)
-                            tc_tma_load_2d(tc_smem_u32(dy_ring + s * kWgDyBytes + k * (kWgK * 128)), &dy_map, n0 + 64 * k, step * kWgK, &sh.full[s]);
-                        if (++t_step == a.steps_per_term) t_step = 0;
-                        if (++s == kWgStages) { s = 0; phase ^= 1u; }
+                            tc_tma_load_2d(tc_smem_u32(dy_ring + s * kWgDyBytes + k * (kWgK * 128)), &dy_map, n0 + 64 * k, step * kWgK, &sh.dy_full[s]);
+                        if (++s == kWgRing) { s = 0; phase ^= 1u; }
                     }
                 }
                 // what is in flight lands before the CTA ends, also after a wait gave up
-                for (uint32_t i = issued > kWgStages ? issued - kWgStages : 0; i < issued; ++i)
+                for (uint32_t i = issued > kWgRing ? issued - kWgRing : 0; i < issued; ++i)
                     for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
-                        if (tc_mbar_try(&sh.full[i % kWgStages], (i / kWgStages) & 1u, 2000u)) break;
+                        if (tc_mbar_try(&sh.dy_full[i % kWgRing], (i / kWgRing) & 1u, 2000u)) break;
             }
             __syncwarp();
         } else if (warp == 17) {
             // -------------------------------------------------------- MMA -------
-            if (rank == 0 && lane == 0) {
-                int s = 0, o = 0;
-                uint32_t phase = 0, chain = 0;
-                bool alive = true;
+            // A wait costs some 250 clocks even when there is nothing to wait for: the barriers of a step are polled by three lanes at once.  The warp stays
+            // together (the MMAs' operands are in uniform registers then) and one elected lane issues.
+            int o = 0;
+            uint32_t phase = 0, chain = 0;
+            bool alive = true;
+            if (rank == 0) {
+                const uint64_t da = wg_desc(tc_smem_u32(wide_ring)), db = wg_desc(tc_smem_u32(dy_ring));
                 for (int item = pair; item < a.items && alive; item += pairs) {
                     const WgItem w = wg_item(a, item, rank);
                     int in_chain = 0;
                     for (int step = w.step0; step < w.step1; ++step) {
                         const uint32_t buf = chain & 1u;
-                        if (in_chain == 0 && !tc_mbar_wait(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        if (!tc_mbar_wait(&sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (in_chain == 0 && !wg_wait_warp<kWgNapMma>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!wg_wait_warp<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
+                            alive = false;
+                            break;
+                        }
+                        tc_fence_async_smem();                   // (see the second CTA's part below)
                         tc_fence_after_sync();
-                        const uint64_t da = wg_desc(tc_smem_u32(wide_ring + o * kWgWideBytes)), db = wg_desc(tc_smem_u32(dy_ring + s * kWgDyBytes));
+                        const bool last = in_chain == kWgChunkSteps - 1 || step + 1 == w.step1;
+                        if (wg_elected()) {
+                            const uint64_t a0 = da + (uint64_t)(o * (kWgWideBytes / 16)), b0 = db + (uint64_t)(o * (kWgDyBytes / 16));
 #pragma unroll
-                        for (int k = 0; k < kWgK / 16; ++k)       // 16 tokens = 2048 bytes on
-                            wg_mma(tmem + buf * kWgN, da + (uint64_t)(k * 128), db + (uint64_t)(k * 128), in_chain || k ? 1u : 0u);
-                        wg_commit_both(&sh.empty[s]);
-                        wg_commit_both(&sh.wide_empty[o]);
-                        if (++in_chain == kWgChunkSteps || step + 1 == w.step1) {
-                            wg_commit_both(&sh.acc_full[buf]);
+                            for (int k = 0; k < kWgK / 16; ++k)       // 16 tokens = 2048 bytes on
+                                wg_mma(tmem + buf * kWgN, a0 + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128), in_chain || k ? 1u : 0u);
+                            wg_commit_both(&sh.done[o]);
+                            if (last) wg_commit_both(&sh.acc_full[buf]);
+                        }
+                        __syncwarp();
+                        ++in_chain;
+                        if (last) {
                             ++chain;
                             in_chain = 0;
                         }
-                        if (++s == kWgStages) s = 0;
-                        if (++o == kWgWide) { o = 0; phase ^= 1u; }
+                        if (++o == kWgRing) { o = 0; phase ^= 1u; }
                     }
                 }
                 // tensor memory is not freed, and no shared memory left, under MMAs in flight
-                wg_commit_own(&sh.drained);
-                for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
-                    if (tc_mbar_try(&sh.drained, 0u, 2000u)) break;
+                if (wg_elected()) {
+                    wg_commit_own(&sh.drained);
+                    for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
+                        if (tc_mbar_try(&sh.drained, 0u, 2000u)) break;
+                }
+                __syncwarp();
+            } else {
+                // The second CTA's steps, told to the first.  The tensor cores read shared memory through the asynchronous proxy; the
+                // fence between the two proxies stands here and before the MMAs, in threads that have nothing in flight: in each of the
+                // widening threads it would wait for that thread's own stores.
+                for (int item = pair; item < a.items && alive; item += pairs) {
+                    const WgItem w = wg_item(a, item, rank);
+                    for (int step = w.step0; step < w.step1; ++step) {
+                        if (!wg_wait_warp<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : &sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        tc_fence_async_smem();
+                        wg_arrive_warp_in_first(&sh.other[o]);
+                        if (++o == kWgRing) { o = 0; phase ^= 1u; }
+                    }
+                }
+            }
+        } else if (warp == 18) {
+            // ------------------------------------------------- copies of codes ----
+            if (lane == 0) {
+                int s = 0;
+                uint32_t phase = 1, issued = 0;
+                bool alive = true;
+                for (int item = pair; item < a.items && alive; item += pairs) {
+                    const WgItem w = wg_item(a, item, rank);
+                    int t_step = w.step0 % a.steps_per_term;
+                    for (int step = w.step0; step < w.step1; ++step, ++issued) {
+                        if (!wg_wait<kWgNapCopy>(&sh.code_empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        tc_mbar_arrive_expect_tx(&sh.code_full[s], kWgCodeBytes);
+                        tc_tma_load_2d(tc_smem_u32(code_ring + s * kWgCodeBytes), &code_map, w.m0, t_step * kWgK, &sh.code_full[s]);
+                        if (++t_step == a.steps_per_term) t_step = 0;
+                        if (++s == kWgCodeRing) { s = 0; phase ^= 1u; }
+                    }
+                }
+                for (uint32_t i = issued > kWgCodeRing ? issued - kWgCodeRing : 0; i < issued; ++i)
+                    for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
+                        if (tc_mbar_try(&sh.code_full[i % kWgCodeRing], (i / kWgCodeRing) & 1u, 2000u)) break;
             }
             __syncwarp();
-        } else if (warp == 18) {
-            // -------------------------------------------------------- scales ----
-            int s = 0;
-            uint32_t phase = 1;
+        } else {
+            // ------------------------------------------------- copies of scales ----
+            int s = 0, told = 0;                         // told: place of the oldest step whose scales have not been announced
+            uint32_t phase = 1, issued = 0;
             bool alive = true;
+            auto tell = [&] {
+                __syncwarp();
+                wg_arrive_warp(&sh.code_full[told]);
+                if (++told == kWgCodeRing) told = 0;
+            };
             for (int item = pair; item < a.items && alive; item += pairs) {
                 const WgItem w = wg_item(a, item, rank);
                 const int block = w.m0 / kCodeBlock;
                 int t_step = w.step0 % a.steps_per_term;
+                // this lane's first word of a step (of a block past the last one: the first word of all, of which nothing is read)
+                const unsigned char *from = a.scales + (block < a.blocks ? ((int64_t)t_step * (kWgK * a.blocks) + lane * a.blocks + block) & ~int64_t(3) : 0);
+                const int per_step = block < a.blocks ? kWgK * a.blocks : 0, per_row = per_step / kWgK;
                 for (int step = w.step0; step < w.step1; ++step) {
-                    if (!tc_mbar_wait_warp(&sh.empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                    const int rows = block < a.blocks ? a.T - t_step * kWgK : 0;         // of the tokens that remain
+                    if (!wg_wait_warp<kWgNapCopy>(&sh.code_empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int t = t_step * kWgK + lane + 32 * k;
-                        const int64_t byte = (int64_t)t * a.blocks + block, word = byte & ~int64_t(3);
-                        const bool in = t < a.T && block < a.blocks;
-                        wg_copy4(tc_smem_u32(&sh.scale[s][lane + 32 * k]), in ? a.scales + word : a.scales,
-                                           in ? (uint32_t)min((int64_t)4, a.scale_bytes - word) : 0u);
+                    for (int k = 0; k < kWgK / 32; ++k) {
+                        const unsigned char *const word = from + 32 * k * per_row;
+                        const bool in = lane + 32 * k < rows;
+                        // (the last word of all may be a part)
+                        wg_copy4(tc_smem_u32(&sh.scale[s][lane + 32 * k]), in ? word : a.scales,
+                                 in ? (uint32_t)min((int64_t)4, a.scale_bytes - (word - a.scales)) : 0u);
                     }
-                    tc_cp_async_arrive(&sh.full[s]);
-                    if (++t_step == a.steps_per_term) t_step = 0;
-                    if (++s == kWgStages) { s = 0; phase ^= 1u; }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (++issued > kWgScalesAhead) {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(kWgScalesAhead) : "memory");
+                        tell();
+                    }
+                    from += per_step;
+                    if (++t_step == a.steps_per_term) { t_step = 0; from -= (int64_t)per_step * a.steps_per_term; }
+                    if (++s == kWgCodeRing) { s = 0; phase ^= 1u; }
                 }
             }
             tc_cp_async_wait_all();
+            for (uint32_t k = 0; k < (issued < kWgScalesAhead ? issued : kWgScalesAhead); ++k) tell();
         }
     }
     tc_fence_before_sync();
