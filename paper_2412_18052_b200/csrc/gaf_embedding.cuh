@@ -5,16 +5,17 @@
 // A token outside 0 .. V-1 is padding: its row of `out` is zero and it adds nothing to any gradient.
 //
 // The gradient is bound by the table: V d elements are written (and read, with a base), while a microbatch touches a few of its
-// rows only.  Every row is written once, by whoever adds it up, so that nothing is cleared first and no atomic touches a sum:
-//   group    positions of equal tokens next to one another: counts, places, positions (one launch of one cluster; the steps
-//            are separated by cluster barriers).  Integer atomics hand out the places, so which position stands where inside a
-//            token's stretch differs from run to run;
-//   order    therefore each stretch is put in ascending order before it is added up: up to 32 positions by the warp that adds
-//            them, longer ones (a few tokens make up much of a text) by one CTA each through a bitmap of the positions;
-//   sum      a warp per row and 1024 columns adds its positions in ascending order in binary32 registers, or writes zeros (or
-//            base).  Stretches of more than 32 positions are cut into pieces of about the square root of their length, which
-//            keeps both the pieces and the sums of a stretch's pieces short chains;
-//   join     adds the pieces of such tokens in order.
+// rows only.  Every row is written once, and no atomic touches a sum.  Two launches:
+//   group + fill   One cluster puts the positions of equal tokens next to one another (counts, places, positions; its steps are
+//            separated by cluster barriers).  Integer atomics hand out the places, so which position stands where inside a token's
+//            stretch differs from run to run; stretches of more than 32 are therefore put in ascending order here (a warp each, a
+//            bit per position), shorter ones by the warp that adds them.  All other CTAs meanwhile write the rows of tokens that do
+//            not occur, each after looking through the tokens for those of its own range of rows.  (Grouping first, then one
+//            kernel that met every row and looked up its count: 67.6 and 479 us where this takes 35 and 324, at 1000
+//            tokens, 50,257 x 768 binary32, and 32,768 tokens, 100,000 x 2048 with a base.)
+//   sum      A warp per occurring token and 256 columns adds its positions in ascending order in binary32 registers.  Stretches of
+//            more than 32 are cut into pieces of about the square root of their length, which keeps both a piece and the sum of a
+//            stretch's pieces a short chain; the warp that finishes a stretch's last piece adds them in order.
 #pragma once
 
 #include "gaf_layer_device.cuh"
@@ -63,17 +64,21 @@ __global__ void __launch_bounds__(kEmbedWarps * 32) embedding_kernel(const Embed
 
 // ---------------------------------------------------------------- gradient --
 
-constexpr int kGroupCtas = 8;                   // one cluster
+constexpr int kGroupCtas = 8;                   // of a cluster
 constexpr int kGroupThreads = 1024;
-constexpr int kLightMost = 32;                  // longest stretch that one warp takes
-constexpr int kOrderThreads = 1024;
-constexpr int kOrderWords = 8192;               // positions whose bits a CTA holds at once, / 32
+constexpr int kLightMost = 32;                  // longest stretch that one warp orders and adds
+constexpr int kOrderWords = 1024;               // positions whose bits a warp holds at once, / 32
+constexpr int kFillRows = 1 << 16;              // rows whose bits a filling CTA holds at once
+constexpr int kGroupSmem = kGroupThreads / 32 * kOrderWords * 4;
+static_assert(kFillRows / 8 <= kGroupSmem, "the bits of the rows fit where the bits of the positions do");
 
-struct Heavy { int v, first_piece, pieces, length; };      // length: positions per piece
-struct Piece { int heavy, index; };
+// A token with a short stretch; a piece of a long one (everything that its sum needs, in one or two loads): its token, first place and
+// positions, which long stretch it belongs to, and that one's pieces.
+struct alignas(16) Light { int v; unsigned int start; int n, unused; };
+struct alignas(16) Piece { int v; unsigned int start; int n, heavy, first_piece, pieces, unused[2]; };
 
-// Words that the grouping kernel clears.
-struct GroupCursors { unsigned int positions, pieces, heavies, reserved; };
+// Words that the grouping cluster clears.
+struct GroupCursors { unsigned int lights, positions, pieces, heavies; };      // (the first two as one 64-bit number, too)
 
 struct EmbedGradArgs {
     const void *dy, *tokens, *base;
@@ -85,12 +90,14 @@ struct EmbedGradArgs {
     unsigned int *slot;         // [T] place of a position inside its token's stretch
     unsigned int *pos;          // [T] positions, stretch by stretch
     unsigned int *ordered;      // [T] the same in ascending order, for long stretches
-    Heavy *heavy;
+    Light *light;
+    unsigned int *heavy;        // tokens with long stretches
     Piece *piece;
+    unsigned int *ticket;       // [long stretch][tile] pieces that are done
     float *partials;            // [piece][d]
-    int64_t dy_stride, V, T, d, parts;
+    int64_t dy_stride, V, T, d, tiles;      // tiles: of a row
     float scale;
-    int piece_ctas;             // CTAs of the summing kernel that take pieces
+    int fillers;                // CTAs of three of the summing kernel that fill rows: 1 or 2
 };
 
 // Positions per piece of a stretch of n > 32: at least 32, about sqrt(n).
@@ -99,14 +106,20 @@ __device__ __forceinline__ int piece_length(unsigned int n) { return max(kLightM
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ unsigned int warp_scan(unsigned int v, int lane) {      // sum of the lanes up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned int below = __shfl_up_sync(0xFFFFFFFFu, v, o);
+        if (lane >= o) v += below;
+    }
+    return v;
+}
 
 template <typename I>
-__global__ void __cluster_dims__(kGroupCtas, 1, 1) __launch_bounds__(kGroupThreads) embedding_group_kernel(const EmbedGradArgs a) {
+__device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned int *smem) {
     constexpr int64_t kThreads = kGroupCtas * kGroupThreads;
     const int64_t tid = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x;
     const int lane = threadIdx.x & 31;
-    grid_wait();
-    grid_release();
     for (int64_t v = tid; v < a.V; v += kThreads) a.count[v] = 0u;
     if (tid == 0) {
         *a.cur = GroupCursors{0u, 0u, 0u, 0u};
@@ -125,214 +138,314 @@ __global__ void __cluster_dims__(kGroupCtas, 1, 1) __launch_bounds__(kGroupThrea
         if (v >= 0) a.slot[t] = first + (unsigned int)__popc(same & ((1u << lane) - 1u));
     }
     cluster_barrier();
-    // places
-    for (int64_t v0 = tid - lane; v0 < a.V; v0 += kThreads) {
-        const int64_t v = v0 + lane;
-        const unsigned int n = v < a.V ? __ldcg(a.count + v) : 0u;
-        if (__ballot_sync(0xFFFFFFFFu, n != 0u) == 0u) continue;
-        unsigned int sum = n;
+    // places; the counts of several rounds together, so that a CTA asks once for all of its tokens (an atomic for each warp and round took most
+    // of this kernel's time: 3000 of them on one address)
+    constexpr int kRounds = 8;
+    __shared__ unsigned long long warp_sum[32];
+    __shared__ unsigned long long cta_first;
+    for (int64_t v00 = tid - threadIdx.x; v00 < a.V; v00 += kRounds * kThreads) {
+        unsigned int counts[kRounds];
+        unsigned long long mine = 0ull;                      // positions of this thread's tokens, and how many short stretches
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int64_t v = v00 + r * kThreads + threadIdx.x;
+            counts[r] = v < a.V ? __ldcg(a.count + v) : 0u;
+        }
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+            mine += ((unsigned long long)counts[r] << 32) + (counts[r] != 0u && counts[r] <= (unsigned int)kLightMost ? 1u : 0u);
+        unsigned long long sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const unsigned int below = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            const unsigned long long below = __shfl_up_sync(0xFFFFFFFFu, sum, o);
             if (lane >= o) sum += below;
         }
-        unsigned int first = 0u;
-        if (lane == 31) first = atomicAdd(&a.cur->positions, sum);
-        first = __shfl_sync(0xFFFFFFFFu, first, 31);
-        if (n != 0u) a.start[v] = first + sum - n;
-        if (n > (unsigned int)kLightMost) {
-            const int length = piece_length(n), pieces = (int)((n + length - 1) / length);
-            const unsigned int h = atomicAdd(&a.cur->heavies, 1u), p = atomicAdd(&a.cur->pieces, (unsigned int)pieces);
-            a.heavy[h] = Heavy{(int)v, (int)p, pieces, length};
-            for (int k = 0; k < pieces; ++k) a.piece[p + k] = Piece{(int)h, k};
+        if (lane == 31) warp_sum[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            unsigned long long s = warp_sum[lane];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned long long below = __shfl_up_sync(0xFFFFFFFFu, s, o);
+                if (lane >= o) s += below;
+            }
+            warp_sum[lane] = s;
+            if (lane == 31) cta_first = atomicAdd(reinterpret_cast<unsigned long long *>(a.cur), s);
         }
+        __syncthreads();
+        const unsigned long long first = cta_first + (threadIdx.x >= 32 ? warp_sum[(threadIdx.x >> 5) - 1] : 0ull) + sum - mine;
+        unsigned int at = (unsigned int)(first >> 32), l = (unsigned int)first;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const unsigned int n = counts[r];
+            if (n == 0u) continue;
+            const int64_t v = v00 + r * kThreads + threadIdx.x;
+            a.start[v] = at;
+            if (n <= (unsigned int)kLightMost) {
+                a.light[l++] = Light{(int)v, at, (int)n, 0};
+            } else {
+                const int length = piece_length(n), pieces = (int)((n + length - 1) / length);
+                const unsigned int h = atomicAdd(&a.cur->heavies, 1u), p = atomicAdd(&a.cur->pieces, (unsigned int)pieces);
+                a.heavy[h] = (unsigned int)v;
+                for (int k = 0; k < pieces; ++k)
+                    a.piece[p + k] = Piece{(int)v, at + (unsigned int)(k * length), min(length, (int)n - k * length), (int)h, (int)p, pieces, {0, 0}};
+                for (int64_t k = 0; k < a.tiles; ++k) a.ticket[h * a.tiles + k] = 0u;
+            }
+            at += n;
+        }
+        __syncthreads();                                     // (the next round's sums go where these were read)
     }
     cluster_barrier();
     for (int64_t t = tid; t < a.T; t += kThreads) {
         const int64_t v = valid_token(static_cast<const I *>(a.tokens), t, a.V);
         if (v >= 0) a.pos[__ldcg(a.start + v) + a.slot[t]] = (unsigned int)t;
     }
-}
-
-// Ascending order of the positions of tokens with more than 32: a bit per position, read back in order.
-__global__ void __launch_bounds__(kOrderThreads) embedding_order_kernel(const EmbedGradArgs a) {
-    __shared__ unsigned int bits[kOrderWords];
-    __shared__ unsigned int warp_total[32];
-    constexpr int kWords = kOrderWords / kOrderThreads;     // consecutive words of a thread
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    grid_wait();
-    grid_release();
-    const unsigned int heavies = a.cur->heavies;
-    for (unsigned int h = blockIdx.x; h < heavies; h += gridDim.x) {
-        const int v = a.heavy[h].v;
-        const unsigned int n = a.count[v], first = a.start[v];
-        unsigned int done = 0u;
+    cluster_barrier();
+    // ascending order of the long stretches: a bit per position, read back in order
+    unsigned int *const bits = smem + (threadIdx.x >> 5) * kOrderWords;
+    const unsigned int heavies = __ldcg(&a.cur->heavies);
+    for (unsigned int h = (unsigned int)(tid >> 5); h < heavies; h += (unsigned int)(kThreads >> 5)) {
+        const unsigned int v = __ldcg(a.heavy + h);
+        const unsigned int n = __ldcg(a.count + v), first = __ldcg(a.start + v);
+        unsigned int done = first;
         for (int64_t t0 = 0; t0 < a.T; t0 += (int64_t)kOrderWords * 32) {
-            for (int w = threadIdx.x; w < kOrderWords; w += kOrderThreads) bits[w] = 0u;
-            __syncthreads();
-            for (unsigned int k = threadIdx.x; k < n; k += kOrderThreads) {
-                const int64_t p = (int64_t)a.pos[first + k] - t0;
+            const int words = (int)min((int64_t)kOrderWords, (a.T - t0 + 31) / 32);
+            for (int w = lane; w < words; w += 32) bits[w] = 0u;
+            __syncwarp();
+            for (unsigned int k = lane; k < n; k += 32) {
+                const int64_t p = (int64_t)__ldcg(a.pos + first + k) - t0;
                 if (p >= 0 && p < (int64_t)kOrderWords * 32) atomicOr(bits + (p >> 5), 1u << (p & 31));
             }
-            __syncthreads();
-            unsigned int word[kWords], mine = 0u;
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                word[k] = bits[threadIdx.x * kWords + k];
-                mine += (unsigned int)__popc(word[k]);
+            __syncwarp();
+            for (int w0 = 0; w0 < words; w0 += 32) {
+                const unsigned int word = w0 + lane < words ? bits[w0 + lane] : 0u;
+                const unsigned int sum = warp_scan((unsigned int)__popc(word), lane);
+                unsigned int at = done + sum - (unsigned int)__popc(word);
+                const unsigned int base = (unsigned int)(t0 + (int64_t)(w0 + lane) * 32);
+                for (unsigned int b = word; b != 0u; b &= b - 1u) a.ordered[at++] = base + (unsigned int)(__ffs(b) - 1);
+                done += __shfl_sync(0xFFFFFFFFu, sum, 31);
             }
-            unsigned int sum = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned int below = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-                if (lane >= o) sum += below;
-            }
-            if (lane == 31) warp_total[warp] = sum;
-            __syncthreads();
-            unsigned int at = first + done + sum - mine, total = 0u;
-            for (int w = 0; w < kOrderThreads / 32; ++w) {
-                const unsigned int c = warp_total[w];
-                if (w < warp) at += c;
-                total += c;
-            }
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                const unsigned int base = (unsigned int)(t0 + (int64_t)(threadIdx.x * kWords + k) * 32);
-                for (unsigned int b = word[k]; b != 0u; b &= b - 1u) a.ordered[at++] = base + (unsigned int)(__ffs(b) - 1);
-            }
-            done += total;
-            __syncthreads();
+            __syncwarp();
         }
     }
 }
 
-// Adds rows of dy to acc: those at the positions that lanes 0 .. n-1 hold, in lane order.
+// One row of a token that does not occur: base, or zeros.  A warp's work.
+template <typename G, bool VEC>
+__device__ __forceinline__ void fill_row(const EmbedGradArgs &a, int64_t v, int lane) {
+    constexpr int kBatch = 4;
+    for (int64_t c0 = 0; c0 < a.d; c0 += kBatch * kTile) {
+        Share<G> s[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            load_tile<VEC>(static_cast<const G *>(a.base) + v * a.d + c0 + k * kTile, lane, a.base ? a.d - c0 - k * kTile : 0, s[k]);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            float x[8];
+            s[k].get(x);
+            store_tile<VEC>(static_cast<G *>(a.grad) + v * a.d + c0 + k * kTile, lane, a.d - c0 - k * kTile, x);
+        }
+    }
+}
+// The first half of the rows is filled beside the grouping, the other half beside the sums.
+__host__ __device__ inline int64_t fill_split(int64_t V) { return V / 2; }
+
+// Rows 0 .. fill_split(V) - 1, while the counts are not known yet.  CTA number `cta` of `ctas`.
+template <typename I, typename G, bool VEC>
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs &a, unsigned int *bits, int64_t cta, int64_t ctas) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t rows = fill_split(a.V), row0 = rows * cta / ctas, row1 = rows * (cta + 1) / ctas;
+    for (int64_t from = row0; from < row1; from += kFillRows) {
+        const int64_t to = min(row1, from + kFillRows);
+        for (int w = threadIdx.x; w < (int)((to - from + 31) / 32); w += kGroupThreads) bits[w] = 0u;
+        __syncthreads();
+        for (int64_t t = threadIdx.x; t < a.T; t += kGroupThreads) {
+            const int64_t v = valid_token(static_cast<const I *>(a.tokens), t, a.V) - from;
+            if (v >= 0 && v < to - from) atomicOr(bits + (v >> 5), 1u << (v & 31));
+        }
+        __syncthreads();
+        for (int64_t v = from + warp; v < to; v += kGroupThreads / 32)
+            if (((bits[(v - from) >> 5] >> ((v - from) & 31)) & 1u) == 0u) fill_row<G, VEC>(a, v, lane);
+        __syncthreads();
+    }
+}
+
+template <typename I, typename G, bool VEC>
+__global__ void __cluster_dims__(kGroupCtas, 1, 1) __launch_bounds__(kGroupThreads, 1) embedding_group_kernel(const EmbedGradArgs a) {
+    extern __shared__ unsigned int group_smem[];
+    grid_wait();
+    grid_release();
+    if (blockIdx.x < kGroupCtas) group_tokens<I>(a, group_smem);
+    // (where base is the output itself, rows that do not occur are right already)
+    else if (a.base != a.grad) fill_rows<I, G, VEC>(a, group_smem, blockIdx.x - kGroupCtas, gridDim.x - kGroupCtas);
+}
+
+// Adds a tile of rows of dy to acc: of those at the positions that lanes 0 .. n-1 hold, in lane order.
 template <typename T, bool VEC>
-__device__ __forceinline__ void add_rows(const EmbedGradArgs &a, unsigned int p, int n, int64_t c0, int lane, float (&acc)[kEmbedTiles][8]) {
-    constexpr int kBatch = sizeof(T) == 4 ? 2 : 4;          // rows in flight
+__device__ __forceinline__ void add_rows(const EmbedGradArgs &a, unsigned int p, int n, int64_t c, int lane, float (&acc)[8]) {
+    constexpr int kBatch = 8;                               // rows in flight
+#pragma unroll 1
     for (int k0 = 0; k0 < n; k0 += kBatch) {
-        Share<T> s[kBatch][kEmbedTiles];
+        Share<T> s[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int64_t t = __shfl_sync(0xFFFFFFFFu, p, (k0 + b) & 31);
-            if (k0 + b < n) {
-#pragma unroll
-                for (int k = 0; k < kEmbedTiles; ++k)
-                    load_tile<VEC>(static_cast<const T *>(a.dy) + t * a.dy_stride + c0 + k * kTile, lane, a.d - c0 - k * kTile, s[b][k]);
-            }
+            if (k0 + b < n) load_tile<VEC>(static_cast<const T *>(a.dy) + t * a.dy_stride + c, lane, a.d - c, s[b]);
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             if (k0 + b >= n) break;
+            float x[8];
+            s[b].get(x);
 #pragma unroll
-            for (int k = 0; k < kEmbedTiles; ++k) {
-                float x[8];
-                s[b][k].get(x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[k][i] += x[i];
-            }
+            for (int i = 0; i < 8; ++i) acc[i] += x[i];
         }
     }
 }
 
 // scale * sum + base, rounded once.
 template <typename G, bool VEC>
-__device__ __forceinline__ void write_row_tile(const EmbedGradArgs &a, int64_t v, int64_t c, int lane, float (&x)[8]) {
-    const int64_t left = a.d - c;
+__device__ __forceinline__ void write_row_tile(const EmbedGradArgs &a, int64_t v, int64_t c, int lane, const Share<G> &base, float (&x)[8]) {
     if (a.base) {
         float b[8];
-        load_tile<VEC>(static_cast<const G *>(a.base) + v * a.d + c, lane, left, b);
+        base.get(b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], a.scale, b[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= a.scale;
     }
-    store_tile<VEC>(static_cast<G *>(a.grad) + v * a.d + c, lane, left, x);
+    store_tile<VEC>(static_cast<G *>(a.grad) + v * a.d + c, lane, a.d - c, x);
 }
 
+// Units of work, a tile of columns each: the pieces of long stretches, then the tokens with short ones.  What leads to a short stretch's rows is
+// fetched ahead, its entry two units and its positions one, so that a unit waits for its rows only.
 template <typename T, typename G, bool VEC>
-__global__ void __launch_bounds__(kEmbedWarps * 32) embedding_sum_kernel(const EmbedGradArgs a) {
+__global__ void __launch_bounds__(kEmbedWarps * 32, 2) embedding_sum_kernel(const EmbedGradArgs a) {
     const int lane = threadIdx.x & 31;
-    float acc[kEmbedTiles][8];
     grid_wait();
     grid_release();
-    if ((int)blockIdx.x < a.piece_ctas) {
-        // pieces of long stretches
-        const int64_t units = (int64_t)a.cur->pieces * a.parts;
-        for (int64_t u = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); u < units; u += (int64_t)a.piece_ctas * kEmbedWarps) {
-            const int64_t p = u / a.parts, c0 = (u - p * a.parts) * kEmbedColumns;
-            const Piece piece = a.piece[p];
-            const Heavy hv = a.heavy[piece.heavy];
-            const unsigned int n_all = a.count[hv.v], from = (unsigned int)piece.index * (unsigned int)hv.length;
-            const int n = (int)min((unsigned int)hv.length, n_all - from);
-            const unsigned int *const at = a.ordered + a.start[hv.v] + from;
-#pragma unroll
-            for (int k = 0; k < kEmbedTiles; ++k)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[k][i] = 0.f;
-            for (int k0 = 0; k0 < n; k0 += 32)
-                add_rows<T, VEC>(a, k0 + lane < n ? at[k0 + lane] : 0u, min(32, n - k0), c0, lane, acc);
-#pragma unroll
-            for (int k = 0; k < kEmbedTiles; ++k)
-                store_tile<VEC>(a.partials + p * a.d + c0 + k * kTile, lane, a.d - c0 - k * kTile, acc[k]);
+    // of every three CTAs the last one or two fill rows
+    const int role = blockIdx.x % 3, summing = 3 - a.fillers;
+    if (role >= summing) {
+        if (a.base == a.grad) return;
+        const int64_t stride = (int64_t)(gridDim.x / 3) * a.fillers * kEmbedWarps * 8;
+        // a warp looks at 8 counts at a time, and fetches the next ones before it writes
+        auto counts = [&](int64_t v0) { return lane < 8 && v0 + lane < a.V ? a.count[v0 + lane] : 1u; };
+        int64_t v0 = fill_split(a.V) + ((int64_t)((blockIdx.x / 3) * a.fillers + role - summing) * kEmbedWarps + (threadIdx.x >> 5)) * 8;
+        unsigned int n = counts(v0);
+        for (; v0 < a.V; v0 += stride) {
+            const unsigned int absent = __ballot_sync(0xFFFFFFFFu, n == 0u);
+            n = counts(v0 + stride);
+            for (unsigned int m = absent; m != 0u; m &= m - 1u) fill_row<G, VEC>(a, v0 + __ffs(m) - 1, lane);
         }
         return;
     }
-    const int64_t unit = (int64_t)(blockIdx.x - a.piece_ctas) * kEmbedWarps + (threadIdx.x >> 5);
-    if (unit >= a.V * a.parts) return;
-    const int64_t v = unit / a.parts, c0 = (unit - v * a.parts) * kEmbedColumns;
-    const unsigned int n = a.count[v];
-    if (n > (unsigned int)kLightMost) return;               // the join writes this row
+    const unsigned int tiles = (unsigned int)a.tiles, warps = gridDim.x / 3 * summing * kEmbedWarps,
+                       me = (blockIdx.x / 3 * summing + role) * kEmbedWarps + (threadIdx.x >> 5);
+    const unsigned int pieces = a.cur->pieces * tiles, lights = a.cur->lights * tiles;
+#pragma unroll 1
+    for (unsigned int u = me; u < pieces; u += warps) {
+        const unsigned int p = u / tiles, tile = u - p * tiles;
+        const int64_t c = (int64_t)tile * kTile;
+        const Piece piece = a.piece[p];
+        const unsigned int *const at = a.ordered + piece.start;
+        float acc[8];
 #pragma unroll
-    for (int k = 0; k < kEmbedTiles; ++k)
+        for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll 1
+        for (int k0 = 0; k0 < piece.n; k0 += 32)
+            add_rows<T, VEC>(a, k0 + lane < piece.n ? at[k0 + lane] : 0u, min(32, piece.n - k0), c, lane, acc);
+        store_tile<VEC>(a.partials + p * a.d + c, lane, a.d - c, acc);
+        // the stretch's last piece to be done: all of them, in order
+        __syncwarp();
+        unsigned int before = 0u;
+        if (lane == 0)
+            asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.ticket + (size_t)piece.heavy * tiles + tile) : "memory");
+        before = __shfl_sync(0xFFFFFFFFu, before, 0);
+        if (before != (unsigned int)piece.pieces - 1u) continue;
+        Share<G> base;
+        if (a.base) load_tile<VEC>(static_cast<const G *>(a.base) + piece.v * a.d + c, lane, a.d - c, base);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[k][i] = 0.f;
-    if (n != 0u) {
-        const unsigned int p = lane < (int)n ? a.pos[a.start[v] + lane] : 0xFFFFFFFFu;
-        unsigned int sorted = p;
-        if (n > 1u) {
+        for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+        const float *const part = a.partials + (int64_t)piece.first_piece * a.d + c;
+        constexpr int kBatch = 8;
+#pragma unroll 1
+        for (int k0 = 0; k0 < piece.pieces; k0 += kBatch) {
+            float s[kBatch][8];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                // (written by other SMs during this launch: from L2)
+                const float *const q = part + (int64_t)(k0 + b) * a.d;
+                if (k0 + b >= piece.pieces) break;
+                if (VEC) {
+                    if (lane * 8 < a.d - c) {
+                        const float4 f = __ldcg(reinterpret_cast<const float4 *>(q + lane * 8)), g = __ldcg(reinterpret_cast<const float4 *>(q + lane * 8) + 1);
+                        s[b][0] = f.x; s[b][1] = f.y; s[b][2] = f.z; s[b][3] = f.w;
+                        s[b][4] = g.x; s[b][5] = g.y; s[b][6] = g.z; s[b][7] = g.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[b][i] = i * 32 + lane < a.d - c ? __ldcg(q + i * 32 + lane) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (k0 + b >= piece.pieces) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] += s[b][i];
+            }
+        }
+        write_row_tile<G, VEC>(a, piece.v, c, lane, base, acc);
+    }
+
+    // (the warps that had no piece, or one less, begin here with the first ones)
+    const unsigned int first = (me + warps - pieces % warps) % warps;
+    auto entry = [&](unsigned int u) { return u < lights ? a.light[u / tiles] : Light{0, 0u, 0, 0}; };
+    auto positions = [&](const Light &x) { return lane < x.n ? a.pos[x.start + lane] : 0xFFFFFFFFu; };
+    Light x = entry(first), next = entry(first + warps);
+    unsigned int p = positions(x);
+#pragma unroll 1
+    for (unsigned int u = first; u < lights; u += warps) {
+        const int64_t c = (int64_t)(u % tiles) * kTile;
+        Share<G> base;
+        if (a.base) load_tile<VEC>(static_cast<const G *>(a.base) + x.v * a.d + c, lane, a.d - c, base);
+        const unsigned int p_next = positions(next);
+        const Light after = entry(u + 2 * warps);
+        float acc[8];
+        if (x.n <= 2) {                                      // most tokens of a text
+            const unsigned int p0 = __shfl_sync(0xFFFFFFFFu, p, 0), p1 = __shfl_sync(0xFFFFFFFFu, p, 1);
+            Share<T> s0, s1;
+            load_tile<VEC>(static_cast<const T *>(a.dy) + (int64_t)min(p0, p1) * a.dy_stride + c, lane, a.d - c, s0);
+            if (x.n == 2) {
+                load_tile<VEC>(static_cast<const T *>(a.dy) + (int64_t)max(p0, p1) * a.dy_stride + c, lane, a.d - c, s1);
+                float y[8];
+                s0.get(acc);
+                s1.get(y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] += y[i];
+            } else {
+                s0.get(acc);
+            }
+        } else {
             int rank = 0;                                    // of this lane's position
-            for (int j = 0; j < (int)n; ++j) rank += __shfl_sync(0xFFFFFFFFu, p, j) < p;
-            for (int j = 0; j < (int)n; ++j) {
+            unsigned int sorted = p;
+#pragma unroll 1
+            for (int j = 0; j < x.n; ++j) rank += __shfl_sync(0xFFFFFFFFu, p, j) < p;
+#pragma unroll 1
+            for (int j = 0; j < x.n; ++j) {
                 const int r = __shfl_sync(0xFFFFFFFFu, rank, j);
                 const unsigned int q = __shfl_sync(0xFFFFFFFFu, p, j);
                 if (r == lane) sorted = q;
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+            add_rows<T, VEC>(a, sorted, x.n, c, lane, acc);
         }
-        add_rows<T, VEC>(a, sorted, (int)n, c0, lane, acc);
-    }
-#pragma unroll
-    for (int k = 0; k < kEmbedTiles; ++k) write_row_tile<G, VEC>(a, v, c0 + k * kTile, lane, acc[k]);
-}
-
-// Rows of tokens with more than 32 positions: their pieces in order.  A warp per row and 256 columns.
-template <typename G, bool VEC>
-__global__ void __launch_bounds__(kEmbedWarps * 32) embedding_join_kernel(const EmbedGradArgs a) {
-    const int lane = threadIdx.x & 31;
-    grid_wait();
-    const int64_t tiles = (a.d + kTile - 1) / kTile, units = (int64_t)a.cur->heavies * tiles;
-    for (int64_t u = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kEmbedWarps) {
-        const int64_t h = u / tiles, c = (u - h * tiles) * kTile;
-        const Heavy hv = a.heavy[h];
-        float acc[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-        const float *const p = a.partials + (int64_t)hv.first_piece * a.d + c;
-        constexpr int kBatch = 4;
-        for (int k0 = 0; k0 < hv.pieces; k0 += kBatch) {
-            Share<float> s[kBatch];
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (k0 + b < hv.pieces) load_tile<VEC>(p + (int64_t)(k0 + b) * a.d, lane, a.d - c, s[b]);
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                if (k0 + b >= hv.pieces) break;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] += s[b].v[i];
-            }
-        }
-        write_row_tile<G, VEC>(a, hv.v, c, lane, acc);
+        write_row_tile<G, VEC>(a, x.v, c, lane, base, acc);
+        x = next;
+        next = after;
+        p = p_next;
     }
 }
 

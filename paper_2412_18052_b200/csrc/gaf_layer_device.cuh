@@ -66,18 +66,38 @@ template <> struct Share<__nv_bfloat16> {
     __device__ __forceinline__ void get(float (&o)[8]) const { unpack_bf16x8(r, o); }
 };
 
+// 32 bytes of one lane, in one access where the address allows it: a warp's two accesses of 16 bytes per lane would each touch half of
+// every 32-byte sector.
+__device__ __forceinline__ void load8_f32(const float *q, float (&v)[8]) {
+    if ((reinterpret_cast<uintptr_t>(q) & 31u) == 0) {
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                     : "l"(q)
+                     : "memory");
+    } else {
+        const float4 a = reinterpret_cast<const float4 *>(q)[0], b = reinterpret_cast<const float4 *>(q)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store8_f32(float *q, const float (&v)[8]) {
+    if ((reinterpret_cast<uintptr_t>(q) & 31u) == 0) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+                     "f"(v[5]), "f"(v[6]), "f"(v[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<float4 *>(q)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(q)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
 // `p`: the tile's first column; `left` columns of the row remain from there on.  What lies past them is zero.
 template <bool VEC>
 __device__ __forceinline__ void load_tile(const float *p, int lane, int64_t left, Share<float> &s) {
     if (VEC) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        if (lane * 8 < left) {
-            const float4 *q = reinterpret_cast<const float4 *>(p + lane * 8);
-            a = q[0];
-            b = q[1];
-        }
-        s.v[0] = a.x; s.v[1] = a.y; s.v[2] = a.z; s.v[3] = a.w;
-        s.v[4] = b.x; s.v[5] = b.y; s.v[6] = b.z; s.v[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s.v[i] = 0.f;
+        if (lane * 8 < left) load8_f32(p + lane * 8, s.v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s.v[i] = i * 32 + lane < left ? p[i * 32 + lane] : 0.f;
@@ -104,11 +124,7 @@ __device__ __forceinline__ void load_tile(const T *p, int lane, int64_t left, fl
 template <bool VEC>
 __device__ __forceinline__ void store_tile(float *p, int lane, int64_t left, const float (&v)[8]) {
     if (VEC) {
-        if (lane * 8 < left) {
-            float4 *q = reinterpret_cast<float4 *>(p + lane * 8);
-            q[0] = make_float4(v[0], v[1], v[2], v[3]);
-            q[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
+        if (lane * 8 < left) store8_f32(p + lane * 8, v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
