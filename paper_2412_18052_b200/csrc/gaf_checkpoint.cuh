@@ -9,8 +9,9 @@
 
 namespace gaf {
 
-constexpr int kCheckpointWarps = 8;
-constexpr int kCheckpointTiles = 4;             // tiles in flight per warp
+constexpr int kCheckpointWarps = 4;
+// Tiles in flight per warp.  (Element by element, each access has a predicate and an address: 1111 columns 71 us with 2, 103 us with 4.)
+__host__ __device__ constexpr int checkpoint_tiles(bool vec) { return vec ? 4 : 2; }
 
 struct CheckpointArgs {
     const void *x;              // pack: the matrix; unpack: written instead (as `out`)
@@ -22,6 +23,7 @@ struct CheckpointArgs {
 
 template <typename T, bool VEC, bool PACK>
 __global__ void __launch_bounds__(kCheckpointWarps * 32) checkpoint_kernel(const CheckpointArgs a) {
+    constexpr int kCheckpointTiles = checkpoint_tiles(VEC);
     const int lane = threadIdx.x & 31;
     const int64_t first = ((int64_t)blockIdx.x * kCheckpointWarps + (threadIdx.x >> 5)) * kCheckpointTiles;
     grid_wait();
@@ -46,8 +48,7 @@ __global__ void __launch_bounds__(kCheckpointWarps * 32) checkpoint_kernel(const
             float v[8];
             unsigned int c[2];
             int e[2];
-            s[k].get(v);
-            encode_tile<VEC>(v, c, e);
+            encode_share<VEC>(s[k], v, c, e);
             store_codes<VEC>(a.codes + rows[k] * a.codes_stride + cols[k], a.scales + rows[k] * a.blocks + cols[k] / kCodeBlock, lane,
                              a.d - cols[k], c, e);
         }

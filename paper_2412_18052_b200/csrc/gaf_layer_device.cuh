@@ -173,13 +173,17 @@ __device__ __forceinline__ float2 value_pair(unsigned short codes) {
     return __half22float2(__half2(h));
 }
 
-// Codes of a warp's tile (two blocks).  c: the lane's 8 codes in order.  e[0], e[1]: the exponents of the blocks of elements 0..3 and 4..7
-// (VEC: both the block of all 8).  Every lane of the warp has to call.
+// Largest magnitudes among a lane's elements, as bits: m[0] of elements 0..3 and m[1] of 4..7 (VEC: m[0] of all).
 template <bool VEC>
-__device__ __forceinline__ void encode_tile(const float (&v)[8], unsigned int (&c)[2], int (&e)[2]) {
-    unsigned int m[2] = {0u, 0u};
+__device__ __forceinline__ void magnitudes(const float (&v)[8], unsigned int (&m)[2]) {
+    m[0] = m[1] = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m[VEC ? 0 : i >> 2] = max(m[VEC ? 0 : i >> 2], __float_as_uint(v[i]) & 0x7FFFFFFFu);
+}
+// Codes of a warp's tile (two blocks).  m: as above.  c: the lane's 8 codes in order.  e[0], e[1]: the exponents of the blocks of elements 0..3
+// and 4..7 (VEC: both the block of all 8).  Every lane of the warp has to call.
+template <bool VEC>
+__device__ __forceinline__ void encode_tile(const float (&v)[8], unsigned int (&m)[2], unsigned int (&c)[2], int (&e)[2]) {
 #pragma unroll
     for (int o = VEC ? 8 : 16; o > 0; o >>= 1) {
         m[0] = max(m[0], __shfl_xor_sync(0xFFFFFFFFu, m[0], o));
@@ -217,6 +221,33 @@ __device__ __forceinline__ void encode_tile(const float (&v)[8], unsigned int (&
     }
     c[0] = (unsigned int)code_pair(x[0], x[1]) | ((unsigned int)code_pair(x[2], x[3]) << 16);
     c[1] = (unsigned int)code_pair(x[4], x[5]) | ((unsigned int)code_pair(x[6], x[7]) << 16);
+}
+template <bool VEC>
+__device__ __forceinline__ void encode_tile(const float (&v)[8], unsigned int (&c)[2], int (&e)[2]) {
+    unsigned int m[2];
+    magnitudes<VEC>(v, m);
+    encode_tile<VEC>(v, m, c, e);
+}
+// The same of a share as it was loaded (v: its elements): packed bfloat16 are compared two at a time.
+template <bool VEC>
+__device__ __forceinline__ void encode_share(const Share<float> &s, float (&v)[8], unsigned int (&c)[2], int (&e)[2]) {
+    s.get(v);
+    encode_tile<VEC>(v, c, e);
+}
+template <bool VEC>
+__device__ __forceinline__ void encode_share(const Share<__nv_bfloat16> &s, float (&v)[8], unsigned int (&c)[2], int (&e)[2]) {
+    s.get(v);
+    const unsigned int p = __vmaxu2(s.r.x & 0x7FFF7FFFu, s.r.y & 0x7FFF7FFFu), q = __vmaxu2(s.r.z & 0x7FFF7FFFu, s.r.w & 0x7FFF7FFFu);
+    unsigned int m[2];
+    if (VEC) {
+        const unsigned int r = __vmaxu2(p, q);
+        m[0] = max(r << 16, r & 0xFFFF0000u);
+        m[1] = 0u;
+    } else {
+        m[0] = max(p << 16, p & 0xFFFF0000u);
+        m[1] = max(q << 16, q & 0xFFFF0000u);
+    }
+    encode_tile<VEC>(v, m, c, e);
 }
 // What a lane's 8 codes stand for; s0, s1: the scales of elements 0..3 and 4..7.
 __device__ __forceinline__ void decode8(const unsigned int (&c)[2], float s0, float s1, float (&v)[8]) {

@@ -80,14 +80,18 @@ template <bool B> struct Flag { static constexpr bool value = B; };
 template <typename F> int by_flag(bool b, F &&f) { return b ? f(Flag<true>()) : f(Flag<false>()); }
 template <int N> struct Count { static constexpr int value = N; };
 
-// Threads per row and tiles per warp of the norm's kernels, by the width alone: as few threads as hold the row in registers.
+// Threads per row and tiles per warp of the norm's kernels, by the width: as few threads as hold the row in registers.  The backward pass has
+// three times as much to hold and takes twice the threads (16384 x 4096 bfloat16: forward 95 us with 128 threads, 103 with 256;
+// backward from codes 105 and 95).
 template <typename F>
-int by_width(int64_t d, F &&f) {
+int by_width(int64_t d, bool backward, F &&f) {
     if (d <= 256) return f(Count<32>(), Count<1>());
+    if (d <= 512) return f(Count<32>(), Count<2>());
+    if (d <= 768) return f(Count<32>(), Count<3>());
     if (d <= 1024) return f(Count<32>(), Count<4>());
     if (d <= 2048) return f(Count<128>(), Count<2>());
-    if (d <= 4096) return f(Count<128>(), Count<4>());
-    if (d <= 8192) return f(Count<256>(), Count<4>());
+    if (d <= 4096) return backward ? f(Count<256>(), Count<2>()) : f(Count<128>(), Count<4>());
+    if (d <= 8192) return backward ? f(Count<512>(), Count<2>()) : f(Count<256>(), Count<4>());
     return f(Count<512>(), Count<4>());
 }
 
@@ -119,29 +123,36 @@ EmbedLayout embed_layout(int64_t T, int64_t d, int64_t V) {
 }
 size_t norm_grad_bytes(int64_t d) { return kLayerScratchOffset + round_up(size_t(kNormMaxCtas) * size_t(d) * 4, 256); }
 
-// How a weight gradient's tokens are split: not at all where the tiles alone fill the device, else into as many parts as do, of
-// whole chains.
-struct WgPlan { int64_t steps_per_term, steps, tiles_m, tiles_n, splits, steps_per_split; };
-WgPlan weight_grad_plan(int64_t T, int64_t N, int64_t M, int dtype, int64_t sms) {
+// How a weight gradient is dealt to `pairs` of CTAs.  Whole tiles as long as they make full rounds; the tiles of a last round that would leave
+// half of the pairs or more without work have their tokens split into as many parts as there are pairs for
+// (16384 x 4096 x 4096 is 256 tiles on 74 pairs: 3 rounds of whole tiles and 34 tiles in halves).
+struct WgPlan { int64_t steps_per_term, steps, tiles_m, tiles_n, whole, rest, splits, steps_per_split; };
+WgPlan weight_grad_plan(int64_t T, int64_t N, int64_t M, int dtype, int64_t pairs) {
     WgPlan p{};
     p.steps_per_term = ceil_div(T, kWgK);
     p.steps = p.steps_per_term * (dtype == GAF_F32 ? 3 : 1);
     p.tiles_m = ceil_div(M, kWgPairM);
     p.tiles_n = ceil_div(N, kWgN);
-    const int64_t chains = ceil_div(p.steps, kWgChunkSteps), tiles = p.tiles_m * p.tiles_n;
-    int64_t splits = tiles > 0 ? sms / 2 / tiles : 1;
-    if (splits > chains) splits = chains;
-    if (splits < 1) splits = 1;
-    p.steps_per_split = ceil_div(chains, splits) * kWgChunkSteps;
-    p.splits = p.steps > 0 ? ceil_div(p.steps, p.steps_per_split) : 1;
+    const int64_t tiles = p.tiles_m * p.tiles_n;
+    p.rest = tiles % pairs;
+    p.splits = p.rest > 0 ? std::min(pairs / p.rest, p.steps) : 1;
+    if (p.splits > 1) {
+        p.steps_per_split = ceil_div(p.steps, p.splits);
+        p.splits = ceil_div(p.steps, p.steps_per_split);
+    }
+    if (p.splits <= 1) {
+        p.splits = 1;
+        p.rest = 0;
+    }
+    p.whole = tiles - p.rest;
     return p;
 }
 struct WgLayout { size_t partials, terms, end; };
 // `relaid`: matrices that dy is laid out anew as.
-WgLayout weight_grad_layout(const WgPlan &p, int64_t N, int64_t M, int relaid) {
+WgLayout weight_grad_layout(const WgPlan &p, int64_t N, int relaid) {
     WgLayout l{};
     l.partials = kLayerScratchOffset;
-    l.terms = l.partials + (p.splits > 1 ? round_up(size_t(p.splits) * size_t(N) * size_t(M) * 4, 256) : 0);
+    l.terms = l.partials + size_t(p.rest * p.splits) * kWgPairM * kWgN * 4;
     l.end = l.terms + round_up(size_t(relaid) * size_t(p.steps_per_term) * kWgK * round_up(size_t(N), 8) * 2, 256);
     return l;
 }
@@ -195,7 +206,7 @@ int launch_embedding_grad(const EmbedGradArgs &a, int dtype, int grad_dtype, int
 }
 
 int launch_rms_norm(const NormArgs &a, int dtype, bool vec, cudaStream_t st) {
-    return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_width(a.d, [&](auto r, auto s) {
+    return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_width(a.d, false, [&](auto r, auto s) {
         constexpr int R = decltype(r)::value;
         const int64_t ctas = ceil_div(a.T, norm_threads(R) / R);
         return launched(launch_dependent(rms_norm_kernel<typename decltype(t)::type, decltype(v)::value, R, decltype(s)::value>, int(ctas),
@@ -205,7 +216,7 @@ int launch_rms_norm(const NormArgs &a, int dtype, bool vec, cudaStream_t st) {
 
 int launch_rms_norm_grad(const NormGradArgs &a, NormFinishArgs f, int dtype, int grad_dtype, bool vec, const DeviceInfo &di, cudaStream_t st) {
     return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_flag(a.h_codes != nullptr, [&](auto coded) {
-        return by_width(a.d, [&](auto r, auto s) {
+        return by_width(a.d, true, [&](auto r, auto s) {
             constexpr int R = decltype(r)::value;
             auto kernel = rms_norm_grad_kernel<typename decltype(t)::type, decltype(v)::value, decltype(coded)::value, R, decltype(s)::value>;
             // as many CTAs as the device holds at once, so that each sums as many rows as possible
@@ -236,7 +247,7 @@ int launch_rms_norm_grad(const NormGradArgs &a, NormFinishArgs f, int dtype, int
 
 template <bool PACK>
 int launch_checkpoint(const CheckpointArgs &a, int dtype, bool vec, cudaStream_t st) {
-    const int64_t ctas = ceil_div(a.n_tiles, int64_t(kCheckpointWarps) * kCheckpointTiles);
+    const int64_t ctas = ceil_div(a.n_tiles, int64_t(kCheckpointWarps) * checkpoint_tiles(vec));
     if (ctas > INT32_MAX) return GAF_ERR_TOO_LARGE;
     return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) {
         return launched(launch_dependent(checkpoint_kernel<typename decltype(t)::type, decltype(v)::value, PACK>, int(ctas), kCheckpointWarps * 32,
@@ -264,7 +275,7 @@ int launch_weight_grad_tiles(const WeightGradArgs &w, const CUtensorMap &dy_map,
         return cudaFuncSetAttribute(weight_grad_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.dyn) == cudaSuccess ? int(GAF_OK)
                                                                                                                           : int(GAF_ERR_CUDA);
     }));
-    const int grid = 2 * std::min(w.items, di.sms / 2);
+    const int grid = 2 * std::min(w.items, int(std::min<int64_t>(di.sms / 2, kWgMaxSplitItems)));
     const cudaError_t err = launch_dependent_smem(weight_grad_kernel<G>, grid, kWgThreads, size_t(kWgSmem), st, w, dy_map, code_map);
     ++*launches;
     return launched(err, *launches);
@@ -278,7 +289,7 @@ int gaf_layer_workspace_bytes(int64_t T, int64_t width, int64_t V, int dtype, si
     if (!bytes_out || !in_range(T) || !in_range(width) || !in_range(V) || !is_dtype(dtype)) return GAF_ERR_ARG;
     // a weight gradient of at most width x width: the partial sums of split tokens are never more than this many tiles
     const int64_t tiles = std::min(kWgMaxSplitItems, ceil_div(width, kWgPairM) * ceil_div(width, kWgN) *
-                                                               ceil_div(ceil_div(T, kWgK) * (dtype == GAF_F32 ? 3 : 1), kWgChunkSteps));
+                                                               ceil_div(T, kWgK) * (dtype == GAF_F32 ? 3 : 1));
     size_t wg = kLayerScratchOffset + size_t(tiles) * kWgPairM * kWgN * 4 + 256;
     wg += size_t(dtype == GAF_F32 ? 3 : 1) * round_up(size_t(T), kWgK) * round_up(size_t(width), 8) * 2;
     const size_t a = embed_layout(T, width, V).end, b = norm_grad_bytes(width);
@@ -467,9 +478,9 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     DeviceInfo di;
     if (!device_info(&di)) return GAF_ERR_CUDA;
     // (a device with more SMs than the workspace was laid out for would split no further)
-    const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms, 2 * kWgMaxSplitItems));
+    const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms / 2, kWgMaxSplitItems));
     if (p.steps * kWgK > kMaxRows || p.tiles_m * p.tiles_n > INT32_MAX / kWgMaxSplitItems) return GAF_ERR_TOO_LARGE;
-    const WgLayout l = weight_grad_layout(p, N, M, relaid);
+    const WgLayout l = weight_grad_layout(p, N, relaid);
     GAF_TRY(check_workspace(workspace, workspace_bytes, l.end));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     int launches = 0;
@@ -480,7 +491,7 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     w.ctl = static_cast<Control *>(workspace);
     w.T = int(T); w.N = N; w.M = M; w.blocks = int(blocks_of(M)); w.scale_bytes = T * blocks_of(M);
     w.steps = int(p.steps); w.steps_per_term = int(std::max<int64_t>(1, p.steps_per_term)); w.steps_per_split = int(p.steps_per_split);
-    w.tiles_m = int(p.tiles_m); w.tiles = int(p.tiles_m * p.tiles_n); w.items = int(p.tiles_m * p.tiles_n * p.splits);
+    w.tiles_m = int(p.tiles_m); w.whole = int(p.whole); w.rest = int(p.rest); w.items = int(p.whole + p.rest * p.splits);
     w.spin_limit = test_wait_limit() ? test_wait_limit() : kTcSpinLimit;
     w.test_extra_arrival = test_withhold() & 1;
 
@@ -513,12 +524,13 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     }
     GAF_TRY(grad_dtype == GAF_F32 ? launch_weight_grad_tiles<float>(w, dy_map, code_map, di, st, &launches)
                                   : launch_weight_grad_tiles<__nv_bfloat16>(w, dy_map, code_map, di, st, &launches));
-    if (p.splits == 1) return GAF_OK;
+    if (p.rest == 0) return GAF_OK;
     WgJoinArgs j{};
-    j.partials = w.partials; j.base = base; j.dweight = dweight; j.elements = N * M; j.splits = p.splits;
-    const int grid = int(ceil_div(j.elements, 1024));
-    const cudaError_t err = grad_dtype == GAF_F32 ? launch_dependent(weight_grad_join_kernel<float>, grid, 256, st, j)
-                                                  : launch_dependent(weight_grad_join_kernel<__nv_bfloat16>, grid, 256, st, j);
+    j.partials = w.partials; j.base = base; j.dweight = dweight; j.N = N; j.M = M;
+    j.splits = int(p.splits); j.tiles_m = int(p.tiles_m); j.whole = int(p.whole); j.rest = int(p.rest);
+    const int grid = int(p.rest) * (kWgPairM * kWgN / kWgJoinElements);
+    const cudaError_t err = grad_dtype == GAF_F32 ? launch_dependent(weight_grad_join_kernel<float>, grid, kWgJoinElements / 4, st, j)
+                                                  : launch_dependent(weight_grad_join_kernel<__nv_bfloat16>, grid, kWgJoinElements / 4, st, j);
     return launched(err, launches + 1);
 }
 

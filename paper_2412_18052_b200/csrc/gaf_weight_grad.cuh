@@ -53,13 +53,14 @@ struct WeightGradArgs {
     const unsigned char *scales;
     const void *base;
     void *dweight;
-    float *partials;            // [split][N][M], when the tokens are split
+    float *partials;            // [split][tile][n][m], of the tiles whose tokens are split
     Control *ctl;
     int64_t N, M, scale_bytes;
     int T, blocks;              // blocks: scale bytes of a row
     int steps, steps_per_term;  // steps of kWgK tokens; of each of the matrices that add up to dy
-    int tiles_m, items;         // items: tiles times splits
-    int tiles, steps_per_split; // (the latter a multiple of kWgChunkSteps)
+    int tiles_m, items;         // items of work: whole tiles, then the parts of the others
+    int whole, rest;            // tiles that are done whole, and the others
+    int steps_per_split;
     unsigned int spin_limit;
     int test_extra_arrival;     // test hook: the first barrier expects an arrival that never comes
 };
@@ -216,15 +217,22 @@ __device__ __forceinline__ void wg_widen16_any(const uint4 &c, unsigned int scal
 }
 
 // A work item: one tile of dW and one range of steps.
-struct WgItem { int m0, n0, split, step0, step1; };             // m0: of this CTA's part
+struct WgItem { int m0, n0, part, step0, step1; };              // m0: of this CTA's half; part: place among the partial sums, or -1
 __device__ __forceinline__ WgItem wg_item(const WeightGradArgs &a, int item, int rank) {
     WgItem w;
-    w.split = item / a.tiles;
-    const int tile = item - w.split * a.tiles, tn = tile / a.tiles_m;
+    int tile = item;
+    w.part = item - a.whole;
+    w.step0 = 0;
+    w.step1 = a.steps;
+    if (w.part >= 0) {
+        const int split = w.part / a.rest;
+        tile = a.whole + w.part - split * a.rest;
+        w.step0 = split * a.steps_per_split;
+        w.step1 = min(a.steps, w.step0 + a.steps_per_split);
+    }
+    const int tn = tile / a.tiles_m;
     w.n0 = tn * kWgN;
     w.m0 = (tile - tn * a.tiles_m) * kWgPairM + rank * kWgM;
-    w.step0 = w.split * a.steps_per_split;
-    w.step1 = min(a.steps, w.step0 + a.steps_per_split);
     return w;
 }
 
@@ -275,11 +283,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     grid_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
 
-    // 5 x 128 threads with 96 registers each: 2 x 160 + 2 x 56 + 48 = 480 (nothing spills: what a thread stores to local memory, its
+    // 5 x 128 threads with 96 registers each: 2 x 168 + 2 x 48 + 48 = 480 (nothing spills: what a thread stores to local memory, its
     // fence for the tensor cores would wait for)
     if (warp < 8) {
         // ------------------------------------------------------------ epilogue ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
         uint32_t chain = 0;
@@ -305,26 +313,25 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 wg_arrive_warp_in_first(&sh.acc_empty[buf]);
             }
             if (!alive) break;
+            if (w.part >= 0) {
+                float *const out = a.partials + ((int64_t)w.part * kWgN + half * 128) * kWgPairM + rank * kWgM + quarter * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < 128; ++j) out[j * kWgPairM] = sum[j];
+                continue;
+            }
             const int64_t m = w.m0 + quarter * 32 + lane, n0 = w.n0 + half * 128;
             if (m < a.M) {
                 const int n = (int)min((int64_t)128, a.N - n0);
-                if (a.items > a.tiles) {
-                    float *const out = a.partials + (w.split * a.N + n0) * a.M + m;
+                const G *const base = static_cast<const G *>(a.base);
+                G *const out = static_cast<G *>(a.dweight) + n0 * a.M + m;
 #pragma unroll
-                    for (int j = 0; j < 128; ++j)
-                        if (j < n) out[j * a.M] = sum[j];
-                } else {
-                    const G *const base = static_cast<const G *>(a.base);
-                    G *const out = static_cast<G *>(a.dweight) + n0 * a.M + m;
-#pragma unroll
-                    for (int j = 0; j < 128; ++j)
-                        if (j < n) out[j * a.M] = from_float<G>(base ? sum[j] + to_float<G>(base[(n0 + j) * a.M + m]) : sum[j]);
-                }
+                for (int j = 0; j < 128; ++j)
+                    if (j < n) out[j * a.M] = from_float<G>(base ? sum[j] + to_float<G>(base[(n0 + j) * a.M + m]) : sum[j]);
             }
         }
     } else if (warp < 16) {
         // ------------------------------------------------------------ widening ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         constexpr int kRows = 8 * (8 / kWgGroups), kUnits = kWgK / kRows;       // rows of a group at a time
         const int group = (warp - 8) / (8 / kWgGroups);
         // A unit is 16 codes of a row.  Four lanes take the four units of half a row (64 codes, one swizzle atom of the widened step), the four
@@ -544,32 +551,35 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     if (sh.abort_flag && threadIdx.x == 0) atomicOr(&a.ctl->status, kStatusTimeoutBit);
 }
 
-// dW = base + the splits' sums in order.  Four elements per thread.
+// dW = base + the parts' sums in order, of the tiles whose tokens were split.  Four elements of a row per thread.
+constexpr int kWgJoinElements = 1024;           // per CTA
 struct WgJoinArgs {
     const float *partials;
     const void *base;
     void *dweight;
-    int64_t elements, splits;
+    int64_t N, M;
+    int splits, tiles_m, whole, rest;
 };
 template <typename G>
-__global__ void __launch_bounds__(256) weight_grad_join_kernel(const WgJoinArgs a) {
-    const int64_t e0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+__global__ void __launch_bounds__(kWgJoinElements / 4) weight_grad_join_kernel(const WgJoinArgs a) {
+    constexpr int kCtas = kWgPairM * kWgN / kWgJoinElements;
+    const int r = blockIdx.x / kCtas, e0 = (blockIdx.x % kCtas) * kWgJoinElements + threadIdx.x * 4;
+    const int tile = a.whole + r, tn = tile / a.tiles_m;
+    const int64_t n = (int64_t)tn * kWgN + e0 / kWgPairM, m = (int64_t)(tile - tn * a.tiles_m) * kWgPairM + e0 % kWgPairM;
     grid_wait();
-    const G *const base = static_cast<const G *>(a.base);
-    G *const out = static_cast<G *>(a.dweight);
-    const int n = (int)min((int64_t)4, a.elements - e0);
-    if (n <= 0) return;
+    if (n >= a.N || m >= a.M) return;
+    const float *p = a.partials + (int64_t)r * (kWgPairM * kWgN) + e0;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if ((a.elements & 3) == 0) {                        // the splits' matrices start on 16-byte boundaries
-        for (int64_t s = 0; s < a.splits; ++s) {
-            const float4 p = __ldcg(reinterpret_cast<const float4 *>(a.partials + s * a.elements + e0));
-            v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
-        }
-    } else {
-        for (int64_t s = 0; s < a.splits; ++s)
-            for (int i = 0; i < n; ++i) v[i] += __ldcg(a.partials + s * a.elements + e0 + i);
+    for (int s = 0; s < a.splits; ++s, p += (int64_t)a.rest * (kWgPairM * kWgN)) {
+        const float4 f = __ldcg(reinterpret_cast<const float4 *>(p));
+        v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
     }
-    for (int i = 0; i < n; ++i) out[e0 + i] = from_float<G>(base ? v[i] + to_float<G>(base[e0 + i]) : v[i]);
+    const G *const base = static_cast<const G *>(a.base);
+    G *const out = static_cast<G *>(a.dweight) + n * a.M + m;
+    const int left = (int)min((int64_t)4, a.M - m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) out[i] = from_float<G>(base ? v[i] + to_float<G>(base[n * a.M + m + i]) : v[i]);
 }
 
 // dy laid out anew where tensor copies cannot read it as it is, as matrices below one another whose rows start on 16-byte boundaries.
