@@ -212,9 +212,16 @@ __device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned in
             const int words = (int)min((int64_t)kOrderWords, (a.T - t0 + 31) / 32);
             for (int w = lane; w < words; w += 32) bits[w] = 0u;
             __syncwarp();
-            for (unsigned int k = lane; k < n; k += 32) {
-                const int64_t p = (int64_t)__ldcg(a.pos + first + k) - t0;
-                if (p >= 0 && p < (int64_t)kOrderWords * 32) atomicOr(bits + (p >> 5), 1u << (p & 31));
+            // (sixteen loads in flight: one after the other, a text's most frequent token took longer than all else here)
+            for (unsigned int k0 = lane; k0 < n; k0 += 32 * 16) {
+                unsigned int at[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) at[j] = k0 + 32 * j < n ? __ldcg(a.pos + first + k0 + 32 * j) : 0xFFFFFFFFu;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int64_t p = (int64_t)at[j] - t0;
+                    if (p >= 0 && p < (int64_t)kOrderWords * 32 && at[j] != 0xFFFFFFFFu) atomicOr(bits + (p >> 5), 1u << (p & 31));
+                }
             }
             __syncwarp();
             for (int w0 = 0; w0 < words; w0 += 32) {
@@ -230,28 +237,33 @@ __device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned in
     }
 }
 
-// One row of a token that does not occur: base, or zeros.  A warp's work.
-template <typename G, bool VEC>
+// One row of a token that does not occur: base, or zeros.  A warp's work; as 16-byte pieces from the first boundary in the row on, whatever the
+// width (base and gradient lie alike), and single elements before and behind.
+template <typename G>
 __device__ __forceinline__ void fill_row(const EmbedGradArgs &a, int64_t v, int lane) {
-    constexpr int kBatch = 4;
-    for (int64_t c0 = 0; c0 < a.d; c0 += kBatch * kTile) {
-        Share<G> s[kBatch];
+    constexpr int kBatch = 8, kPer = 16 / sizeof(G);
+    G *const out = static_cast<G *>(a.grad) + v * a.d;
+    const G *const in = static_cast<const G *>(a.base) + v * a.d;
+    const int64_t head = min(a.d, (int64_t)(((16u - (unsigned int)(reinterpret_cast<uintptr_t>(out) & 15u)) & 15u) / sizeof(G)));
+    const int64_t pieces = (a.d - head) / kPer, tail = head + pieces * kPer;
+    if (lane < head) out[lane] = a.base ? in[lane] : from_float<G>(0.f);
+    if (tail + lane < a.d) out[tail + lane] = a.base ? in[tail + lane] : from_float<G>(0.f);
+    uint4 *const to = reinterpret_cast<uint4 *>(out + head);
+    const uint4 *const from = reinterpret_cast<const uint4 *>(in + head);
+    for (int64_t c0 = lane; c0 < pieces; c0 += 32 * kBatch) {
+        uint4 x[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) x[k] = a.base && c0 + 32 * k < pieces ? from[c0 + 32 * k] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
-            load_tile<VEC>(static_cast<const G *>(a.base) + v * a.d + c0 + k * kTile, lane, a.base ? a.d - c0 - k * kTile : 0, s[k]);
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            float x[8];
-            s[k].get(x);
-            store_tile<VEC>(static_cast<G *>(a.grad) + v * a.d + c0 + k * kTile, lane, a.d - c0 - k * kTile, x);
-        }
+            if (c0 + 32 * k < pieces) to[c0 + 32 * k] = x[k];
     }
 }
 // The first half of the rows is filled beside the grouping, the other half beside the sums.
 __host__ __device__ inline int64_t fill_split(int64_t V) { return V / 2; }
 
 // Rows 0 .. fill_split(V) - 1, while the counts are not known yet.  CTA number `cta` of `ctas`.
-template <typename I, typename G, bool VEC>
+template <typename I, typename G>
 __device__ __forceinline__ void fill_rows(const EmbedGradArgs &a, unsigned int *bits, int64_t cta, int64_t ctas) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t rows = fill_split(a.V), row0 = rows * cta / ctas, row1 = rows * (cta + 1) / ctas;
@@ -265,19 +277,19 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs &a, unsigned int *
         }
         __syncthreads();
         for (int64_t v = from + warp; v < to; v += kGroupThreads / 32)
-            if (((bits[(v - from) >> 5] >> ((v - from) & 31)) & 1u) == 0u) fill_row<G, VEC>(a, v, lane);
+            if (((bits[(v - from) >> 5] >> ((v - from) & 31)) & 1u) == 0u) fill_row<G>(a, v, lane);
         __syncthreads();
     }
 }
 
-template <typename I, typename G, bool VEC>
+template <typename I, typename G>
 __global__ void __cluster_dims__(kGroupCtas, 1, 1) __launch_bounds__(kGroupThreads, 1) embedding_group_kernel(const EmbedGradArgs a) {
     extern __shared__ unsigned int group_smem[];
     grid_wait();
     grid_release();
     if (blockIdx.x < kGroupCtas) group_tokens<I>(a, group_smem);
     // (where base is the output itself, rows that do not occur are right already)
-    else if (a.base != a.grad) fill_rows<I, G, VEC>(a, group_smem, blockIdx.x - kGroupCtas, gridDim.x - kGroupCtas);
+    else if (a.base != a.grad) fill_rows<I, G>(a, group_smem, blockIdx.x - kGroupCtas, gridDim.x - kGroupCtas);
 }
 
 // Adds a tile of rows of dy to acc: of those at the positions that lanes 0 .. n-1 hold, in lane order.
@@ -337,7 +349,7 @@ __global__ void __launch_bounds__(kEmbedWarps * 32, 2) embedding_sum_kernel(cons
         for (; v0 < a.V; v0 += stride) {
             const unsigned int absent = __ballot_sync(0xFFFFFFFFu, n == 0u);
             n = counts(v0 + stride);
-            for (unsigned int m = absent; m != 0u; m &= m - 1u) fill_row<G, VEC>(a, v0 + __ffs(m) - 1, lane);
+            for (unsigned int m = absent; m != 0u; m &= m - 1u) fill_row<G>(a, v0 + __ffs(m) - 1, lane);
         }
         return;
     }
@@ -369,7 +381,7 @@ __global__ void __launch_bounds__(kEmbedWarps * 32, 2) embedding_sum_kernel(cons
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = 0.f;
         const float *const part = a.partials + (int64_t)piece.first_piece * a.d + c;
-        constexpr int kBatch = 8;
+        constexpr int kBatch = 4;
 #pragma unroll 1
         for (int k0 = 0; k0 < piece.pieces; k0 += kBatch) {
             float s[kBatch][8];

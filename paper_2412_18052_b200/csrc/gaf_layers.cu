@@ -176,7 +176,7 @@ int launch_embedding_grad(const EmbedGradArgs &a, int dtype, int grad_dtype, int
         typedef typename std::conditional<decltype(i64)::value, int64_t, int32_t>::type I;
         typedef typename decltype(g)::type G;
         constexpr bool kVec = decltype(v)::value;
-        auto group = embedding_group_kernel<I, G, kVec>;
+        auto group = embedding_group_kernel<I, typename decltype(g)::type>;
         auto sum_f32 = embedding_sum_kernel<float, G, kVec>;
         auto sum_bf16 = embedding_sum_kernel<__nv_bfloat16, G, kVec>;
         // as many clusters, and as many CTAs that sum, as the device holds at once
