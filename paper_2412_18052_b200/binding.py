@@ -271,10 +271,9 @@ def gaf_layer_workspace_bytes(T: int, width: int, dtype: int, V: int = 0) -> int
 
 def new_layer_workspace(T: int, width: int, dtype: int, V: int = 0, device=None) -> torch.Tensor:
     """Workspace of the layers' gradients for up to T tokens, matrices of up to ``width`` columns and tables of V rows
-    (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter."""
-    ws = torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
-    gaf_workspace_init(ws)
-    return ws
+    (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter (but to the filter: a workspace that
+    is to serve both goes through gaf_workspace_init once)."""
+    return torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
 
 
 Checkpoint = Tuple[torch.Tensor, torch.Tensor]

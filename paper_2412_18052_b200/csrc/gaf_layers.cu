@@ -479,7 +479,8 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     if (!device_info(&di)) return GAF_ERR_CUDA;
     // (a device with more SMs than the workspace was laid out for would split no further)
     const WgPlan p = weight_grad_plan(T, N, M, dtype, std::min<int64_t>(di.sms / 2, kWgMaxSplitItems));
-    if (p.steps * kWgK > kMaxRows || p.tiles_m * p.tiles_n > INT32_MAX / kWgMaxSplitItems) return GAF_ERR_TOO_LARGE;
+    // (tile coordinates are 32 bits)
+    if (N > kMaxRows - kWgPairM || M > kMaxRows - kWgPairM || p.steps * kWgK > kMaxRows || p.tiles_m * p.tiles_n > INT32_MAX / kWgMaxSplitItems) return GAF_ERR_TOO_LARGE;
     const WgLayout l = weight_grad_layout(p, N, relaid);
     GAF_TRY(check_workspace(workspace, workspace_bytes, l.end));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -492,7 +493,7 @@ int gaf_linear_weight_grad(const void *dy, int64_t dy_stride, int dtype, const u
     w.T = int(T); w.N = N; w.M = M; w.blocks = int(blocks_of(M)); w.scale_bytes = T * blocks_of(M);
     w.steps = int(p.steps); w.steps_per_term = int(std::max<int64_t>(1, p.steps_per_term)); w.steps_per_split = int(p.steps_per_split);
     w.tiles_m = int(p.tiles_m); w.whole = int(p.whole); w.rest = int(p.rest); w.items = int(p.whole + p.rest * p.splits);
-    w.spin_limit = test_wait_limit() ? test_wait_limit() : kTcSpinLimit;
+    w.spin_limit = test_wait_limit() ? test_wait_limit() : kWgSpinLimit;
     w.test_extra_arrival = test_withhold() & 1;
 
     CUtensorMap dy_map{}, code_map{};

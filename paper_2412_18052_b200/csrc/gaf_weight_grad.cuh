@@ -48,6 +48,7 @@ constexpr uint32_t kWgScalesAhead = 1;                  // steps whose scales ar
 constexpr int kWgThreads = 640;
 constexpr int kWgNapEpilogue = 400, kWgNapWiden = 0, kWgNapCopy = 100, kWgNapMma = 0;
 constexpr int kWgTmemCols = 512;
+constexpr unsigned int kWgSpinLimit = 1u << 23;         // attempts of tens of clocks each: a third of a second or more
 
 struct WeightGradArgs {
     const unsigned char *scales;

@@ -27,6 +27,10 @@ The five named configurations:
   4  K=8  D=124,439,808   fp32  rho ~ N(0.02, 0.05^2), tau=0.97
   5  K=8  D=1,000,000,000 bf16  rho ~ 50% U(0.3, 0.8) / 50% U(-0.3, 0.1), tau=0.97
 
+Beside the mixtures, ``LanguageModel`` makes real micro-gradients: one microbatch after another through a small language
+model whose memory-bound layers, 8-bit checkpoints and weight gradients are the library's own (``gaf_embedding`` and
+its neighbours), each weight's gradient written straight into its slice of a flat buffer.
+
 Configuration n uses seed n-1.  rho values are drawn first, from a CPU generator,
 so they do not depend on the device; the vectors are drawn on the requested
 device (CPU and GPU streams differ, which is fine: both consumers see the same
@@ -177,4 +181,86 @@ def config(n: int, device: str = "cpu", D: Optional[int] = None,
                                         torch.tensor(sizes)).to(device)
     w = Workload(f"config{n}", K_, D_, dtype, taus, rho, seed)
     w.grads = _draw(K_, D_, dtype, rho, seed, device, sigma, stacked=stacked)
+    return w
+
+
+class LanguageModel:
+    """Token embedding (scaled by sqrt(d)), RMS norm, a linear layer, RMS norm after the residual's addition, and the table once
+    more as the output layer, under a cross-entropy loss: the smallest language model in which every layer operator of the library has its
+    place.  The matrix products of the forward pass, the products that carry a gradient back through a linear layer, and the loss are
+    plain torch.
+
+    ``sizes``: name and shape of each weight; weight i starts at ``offsets[i]`` of a flat gradient (multiples of 8 elements, so
+    that the offsets serve ``gaf_filter_accumulate_bucketed`` too); D: the flat gradient's length.
+    """
+
+    def __init__(self, V: int, d: int, seed: int = 0, dtype: torch.dtype = torch.bfloat16, device: str = "cuda"):
+        gen = torch.Generator(device=device)
+        gen.manual_seed(seed)
+
+        def draw(*shape, size, mean=0.0):
+            return (mean + size * torch.randn(*shape, generator=gen, device=device)).to(dtype)
+        self.V, self.d, self.dtype, self.device = V, d, dtype, device
+        self.table = draw(V, d, size=0.3)
+        self.w1, self.w2 = draw(d, size=0.1, mean=1.0), draw(d, size=0.1, mean=1.0)
+        self.lin = draw(d, d, size=d ** -0.5)
+        self.sizes = [("table", (V, d)), ("w1", (d,)), ("lin", (d, d)), ("w2", (d,))]
+        self.offsets = [0]
+        for _, shape in self.sizes:
+            self.offsets.append(self.offsets[-1] + (math.prod(shape) + 7) // 8 * 8)
+        self.D = self.offsets[-1]
+
+    def views(self, flat: torch.Tensor) -> dict:
+        """The weights' slices of a flat gradient, by name."""
+        return {name: flat[at:at + math.prod(shape)].view(shape) for (name, shape), at in zip(self.sizes, self.offsets)}
+
+    def new_workspace(self, T: int) -> torch.Tensor:
+        from . import binding
+        code = binding.GAF_F32 if self.dtype == torch.float32 else binding.GAF_BF16
+        return binding.new_layer_workspace(T, max(self.V, self.d), code, V=self.V, device=self.device)
+
+    def tokens(self, T: int, seed: int) -> torch.Tensor:
+        """T tokens after Zipf's law, the last few padding (-1)."""
+        gen = torch.Generator(device=self.device)
+        gen.manual_seed(seed)
+        u = torch.rand(T, generator=gen, device=self.device, dtype=torch.float64)
+        t = (torch.exp(u * math.log(self.V + 1)).to(torch.int64) - 1).clamp(0, self.V - 1)
+        t[T - T // 30:] = -1
+        return t
+
+    def micro_gradient(self, tokens: torch.Tensor, targets: torch.Tensor, flat: torch.Tensor, workspace: torch.Tensor) -> dict:
+        """Forward and backward pass of one microbatch: the gradient into ``flat`` (float32 or bfloat16, all slices written).  Between the
+        passes only 8-bit checkpoints of the activations are kept.  Returns the activations and their gradients by name (for
+        tests: a training step has no use for them)."""
+        from . import binding as gaf
+        g, T, scale = self.views(flat), tokens.numel(), math.sqrt(self.d)
+        y1c, h1c, y2c, h2c = (gaf.new_checkpoint(T, self.d, self.device) for _ in range(4))
+        e = gaf.gaf_embedding(self.table, tokens, scale=scale)
+        y1, _, r1 = gaf.gaf_rms_norm(e, self.w1, y_checkpoint=y1c, coded_y=True, h_checkpoint=h1c)
+        z = (y1.float() @ self.lin.float().t()).to(self.dtype)
+        y2, h2, r2 = gaf.gaf_rms_norm(z, self.w2, residual=e, y_checkpoint=y2c, coded_y=True, h_checkpoint=h2c)
+        dlogits = torch.softmax(y2.float() @ self.table.float().t(), dim=1)
+        dlogits[torch.arange(T, device=self.device), targets] -= 1.0
+        dlogits = (dlogits.masked_fill((tokens < 0)[:, None], 0.0) / T).to(self.dtype)
+        gaf.gaf_linear_weight_grad(dlogits, y2c, g["table"], workspace)
+        dy2 = (dlogits.float() @ self.table.float()).to(self.dtype)
+        dh2, _ = gaf.gaf_rms_norm_grad(dy2, h2c, self.w2, r2, g["w2"], workspace)
+        gaf.gaf_linear_weight_grad(dh2, y1c, g["lin"], workspace)
+        dy1 = (dh2.float() @ self.lin.float()).to(self.dtype)
+        de, _ = gaf.gaf_rms_norm_grad(dy1, h1c, self.w1, r1, g["w1"], workspace, residual_grad=dh2)
+        gaf.gaf_embedding_grad(de, tokens, g["table"], workspace, scale=scale, base=g["table"])
+        return dict(tokens=tokens, e=e, y1=y1, h2=h2, y2=y2, r1=r1, r2=r2, dlogits=dlogits, dy2=dy2, dh2=dh2, dy1=dy1, de=de,
+                    y1c=y1c, y2c=y2c, h1c=h1c, h2c=h2c)
+
+
+def language_model(K: int, V: int, d: int, T: int, seed: int = 0, dtype: str = "f32", taus: Sequence[float] = (0.97,)) -> Workload:
+    """K micro-gradients of a ``LanguageModel`` on microbatches of T tokens, made on the GPU by the library's layers."""
+    model = LanguageModel(V, d, seed)
+    w = Workload("language_model", K, model.D, dtype, [float(t) for t in taus], [], seed)
+    workspace, tdtype = model.new_workspace(T), torch.float32 if dtype == "f32" else torch.bfloat16
+    for k in range(K):
+        flat = torch.zeros(model.D, dtype=tdtype, device=model.device)
+        tokens = model.tokens(T, seed * 1000 + 2 * k)
+        model.micro_gradient(tokens, model.tokens(T, seed * 1000 + 2 * k + 1).clamp(min=0), flat, workspace)
+        w.grads.append(flat)
     return w

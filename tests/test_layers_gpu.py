@@ -461,47 +461,7 @@ def test_linear_weight_grad_bounded_waits():
 
 # ---------------------------------------------------------------- together ----
 
-class Model:
-    """Token embedding, two norms with a linear layer between them, the table once more as the output layer: one microbatch after another
-    into flat micro-gradients, as a training step does it.  What the library does not have (products, the loss) is plain torch."""
-    def __init__(self, V, d, seed, t=torch.bfloat16):
-        g = gen(seed)
-        self.V, self.d, self.t = V, d, t
-        self.table, self.w1, self.w2 = randn(g, V, d, dtype=t, size=0.3), 1 + randn(g, d, dtype=t, size=0.1), 1 + randn(g, d, dtype=t, size=0.1)
-        self.lin = randn(g, d, d, dtype=t, size=d ** -0.5)
-        self.sizes = [("table", (V, d)), ("w1", (d,)), ("lin", (d, d)), ("w2", (d,))]
-        self.D = sum((math.prod(s) + 7) // 8 * 8 for _, s in self.sizes)
-
-    def views(self, flat):
-        out, at = {}, 0
-        for name, s in self.sizes:
-            out[name] = flat[at:at + math.prod(s)].view(s)
-            at += (math.prod(s) + 7) // 8 * 8
-        return out
-
-    def micro_gradient(self, tokens, targets, flat, ws):
-        """The library's calls, the activations kept in 8 bits."""
-        g, T = self.views(flat), tokens.numel()
-        scale = math.sqrt(self.d)
-        e = gaf.gaf_embedding(self.table, tokens, scale=scale)
-        y1c, h1c, y2c, h2c = (gaf.new_checkpoint(T, self.d) for _ in range(4))
-        y1, _, r1 = gaf.gaf_rms_norm(e, self.w1, y_checkpoint=y1c, coded_y=True, h_checkpoint=h1c)
-        z = (y1.float() @ self.lin.float().t()).to(self.t)
-        y2, h2, r2 = gaf.gaf_rms_norm(z, self.w2, residual=e, y_checkpoint=y2c, coded_y=True, h_checkpoint=h2c)
-        logits = y2.float() @ self.table.float().t()
-        dlogits = torch.softmax(logits, dim=1)
-        dlogits[torch.arange(T, device="cuda"), targets] -= 1.0
-        dlogits = dlogits.masked_fill((tokens < 0)[:, None], 0.0)
-        dlogits = (dlogits / T).to(self.t)
-        gaf.gaf_linear_weight_grad(dlogits, y2c, g["table"], ws)
-        dy2 = (dlogits.float() @ self.table.float()).to(self.t)
-        dh2, _ = gaf.gaf_rms_norm_grad(dy2, h2c, self.w2, r2, g["w2"], ws)
-        gaf.gaf_linear_weight_grad(dh2, y1c, g["lin"], ws)
-        dy1 = (dh2.float() @ self.lin.float()).to(self.t)
-        de, _ = gaf.gaf_rms_norm_grad(dy1, h1c, self.w1, r1, g["w1"], ws, residual_grad=dh2)
-        gaf.gaf_embedding_grad(de, tokens, g["table"], ws, scale=scale, base=g["table"])
-        return dict(tokens=tokens, e=e, y1=y1, h2=h2, y2=y2, r1=r1, r2=r2, dlogits=dlogits, dy2=dy2, dh2=dh2, dy1=dy1, de=de, y1c=y1c, y2c=y2c, h1c=h1c, h2c=h2c)
-
+class Model(workloads.LanguageModel):
     def check(self, s, flat):
         """Every gradient against binary64, from the activations and gradients that the step itself had."""
         g = self.views(flat)
@@ -518,21 +478,34 @@ class Model:
         assert_close(g["table"], out_layer + table, o1 + o2 + 4 * ref.U * (out_layer.abs() + table.abs()), "table")
 
 
-def test_micro_gradients_of_a_language_model_are_filtered():
-    K, T, V, d = 4, 200, 600, 264
-    m = Model(V, d, 3)
-    ws = gaf.new_layer_workspace(T, max(V, d), gaf.GAF_BF16, V=V)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [600, 301])
+def test_micro_gradients_of_a_language_model_are_filtered(V, dtype):
+    K, T, d = 4, 200, 264
+    m = Model(V, d, 3, dtype=TYPES[dtype])
+    ws = m.new_workspace(T)
     flats, g = [torch.zeros(m.D, device="cuda") for _ in range(K)], gen(77)
-    for flat in flats:
-        tokens = zipf(g, T, V)
-        tokens[-7:] = -1
-        m.check(m.micro_gradient(tokens, torch.randint(0, V, (T,), generator=g, device="cuda"), flat, ws), flat)
+    for k, flat in enumerate(flats):
+        m.check(m.micro_gradient(m.tokens(T, k), torch.randint(0, V, (T,), generator=g, device="cuda"), flat, ws), flat)
     filter_ws = gaf.new_workspace(K, m.D, gaf.GAF_F32)
     macro, mask, dist, count = gaf.gaf_filter_accumulate(flats, 0.97, filter_ws)
     want = orc.filter_accumulate([workloads.as_numpy_bits(f) for f in flats], 0.97)
     near = abs(want.dist - 0.97) < 1e-5
     assert not near.any() and mask.cpu().numpy().tolist() == want.mask.tolist() and int(count.item()) == want.count
     assert float(abs(dist.cpu().numpy() - want.dist).max()) < 1e-5
+
+
+def test_language_model_workload():
+    """The workload's micro-gradients, in both types, through the filter and its bucketed form."""
+    for dtype, code in (("f32", gaf.GAF_F32), ("bf16", gaf.GAF_BF16)):
+        w = workloads.language_model(3, 500, 128, 150, seed=2, dtype=dtype)
+        want = orc.filter_accumulate([workloads.as_numpy_bits(f) for f in w.grads], 0.97)
+        ws = gaf.new_workspace(w.K, w.D, code)
+        macro, mask, dist, count = gaf.gaf_filter_accumulate(w.grads, 0.97, ws)
+        assert float(abs(dist.cpu().numpy() - want.dist).max()) < 1e-5 and mask.cpu().numpy().tolist() == want.mask.tolist()
+        offsets = workloads.LanguageModel(500, 128, 2).offsets
+        _, m, _, c = gaf.gaf_filter_accumulate_bucketed(w.grads, 0.97, offsets, ws)
+        assert m.shape == (4, 3) and bool((c >= 1).all())
 
 
 def test_one_workspace_serves_layers_and_filter():
