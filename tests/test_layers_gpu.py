@@ -585,3 +585,115 @@ def test_binding_refusals():
                  lambda: gaf.gaf_embedding(x.flatten()[1:65].view(1, 64), tokens), lambda: gaf.gaf_checkpoint_pack(x, (ck[0].flatten()[:4 * 40].view(4, 40), ck[1]))):
         with pytest.raises((gaf.GafError, ValueError)):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_is_written_outside_a_workspace(dtype):
+    """A workspace of exactly the size asked for: what lies before and behind it, and what the filter keeps in it, stays as it was."""
+    t, g = TYPES[dtype], gen(40)
+    code = gaf.GAF_F32 if dtype == "f32" else gaf.GAF_BF16
+    for T, width, V in ((1, 1, 1), (40, 300, 20), (3000, 264, 50), (700, 1000, 3000)):
+        n = gaf.gaf_layer_workspace_bytes(T, width, code, V)
+        room = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+        ws = room[1024:1024 + n]
+        d = width
+        dy, tokens = randn(g, T, d, dtype=t), zipf(g, T, V)
+        gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws)
+        h, w = randn(g, T, d, dtype=t), randn(g, d, dtype=t)
+        gaf.gaf_rms_norm_grad(dy, h, w, torch.ones(T, device="cuda"), torch.empty(d, device="cuda"), ws)
+        gaf.gaf_linear_weight_grad(dy, gaf.gaf_checkpoint_pack(h), torch.empty(d, d, device="cuda"), ws)
+        assert gaf.gaf_read_status(ws) == 0
+        assert bool((room[:1024] == 77).all()) and bool((room[1024 + n:] == 77).all())
+        kept = room[1024:1024 + 53248 + 138240]          # control block, partial sums, words that CTAs exchange
+        assert int((kept != 77).sum()) <= 4              # (the status word)
+        with pytest.raises(gaf.GafError):
+            gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws[:1024])
+
+
+def test_two_streams_and_two_graphs_at_once():
+    """The same work on two streams side by side, and two captured graphs replayed together, each with a workspace of its own."""
+    T, V, d = 700, 900, 520
+    m = Model(V, d, 8)
+    g = gen(80)
+    batches = [(m.tokens(T, 50 + k), torch.randint(0, V, (T,), generator=g, device="cuda")) for k in range(2)]
+    spaces = [m.new_workspace(T) for _ in range(2)]
+    want = []
+    for tokens, targets in batches:
+        flat = torch.zeros(m.D, device="cuda")
+        m.micro_gradient(tokens, targets, flat, spaces[0])
+        want.append(flat)
+    torch.cuda.synchronize()
+    streams, flats = [torch.cuda.Stream() for _ in range(2)], [torch.zeros(m.D, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                flats[k].zero_()
+                m.micro_gradient(*batches[k], flats[k], spaces[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(flats, want))
+    graphs = []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            m.micro_gradient(*batches[k], flats[k], spaces[k])
+        graphs.append(graph)
+    for _ in range(3):
+        for f in flats:
+            f.zero_()
+        torch.cuda.synchronize()
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                graphs[k].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(flats, want))
+
+
+def test_everything_is_reproducible():
+    """Bit for bit, call after call, whatever ran in between."""
+    g = gen(90)
+    T, d, V, N = 3000, 776, 400, 520
+    dy, h, w, tokens = randn(g, T, d, dtype=torch.bfloat16), randn(g, T, d, dtype=torch.bfloat16), randn(g, d, dtype=torch.bfloat16), zipf(g, T, V)
+    dyn, rstd, ck = randn(g, T, N, dtype=torch.bfloat16), torch.ones(T, device="cuda"), gaf.gaf_checkpoint_pack(h)
+    ws = workspace(T, d, torch.bfloat16, V=V)
+
+    def run():
+        a = gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws)
+        b = gaf.gaf_rms_norm_grad(dy, ck, w, rstd, torch.empty(d, device="cuda"), ws)
+        c = gaf.gaf_linear_weight_grad(dyn, ck, torch.empty(N, d, device="cuda"), ws)
+        return [a, *b, c]
+    first = run()
+    for _ in range(5):
+        ws.random_()
+        assert all(torch.equal(x, y) for x, y in zip(run(), first))
+
+
+def test_dense_neighbours_of_every_alignment():
+    """Weights' slices at every place of a flat gradient that the library takes: multiples of 16 bytes that are none of 32."""
+    g = gen(91)
+    T, d, V = 300, 264, 120
+    dy, tokens = randn(g, T, d), zipf(g, T, V)
+    h, w, rstd, ck = randn(g, T, d), randn(g, d), torch.ones(T, device="cuda"), gaf.gaf_checkpoint_pack(randn(g, T, d))
+    ws = workspace(T, d, torch.float32, V=V)
+    for gt, shift in ((torch.float32, 4), (torch.float32, 8), (torch.bfloat16, 8), (torch.bfloat16, 24)):
+        flat = torch.full((V * d + 2 * d * d + 200,), 7.0, dtype=gt, device="cuda")
+        a, b = flat[shift:shift + V * d].view(V, d), flat[V * d + 40 + shift:V * d + 40 + shift + d]
+        c = flat[V * d + d + 80 + shift:V * d + d + 80 + shift + d * d].view(d, d)
+        gaf.gaf_embedding_grad(dy, tokens, a, ws)
+        assert_close(a, *ref.embedding_grad(dy, tokens, V, 1.0))
+        _, dw = gaf.gaf_rms_norm_grad(dy, h, w, rstd, b, ws)
+        _, want, _, off = ref.rms_norm_grad(dy, h.double(), w, rstd)
+        assert_close(b, want, off)
+        gaf.gaf_linear_weight_grad(dy, ck, c, ws)
+        assert_close(c, *ref.weight_grad(dy, ref.checkpoint_values(ck)))
+        used = torch.zeros_like(flat, dtype=torch.bool)
+        for v in (a, b, c):
+            lo = (v.data_ptr() - flat.data_ptr()) // flat.element_size()
+            used[lo:lo + v.numel()] = True
+        assert bool((flat[~used] == 7.0).all())
+    # matrices whose rows are 16 bytes, not 32, from a boundary
+    x = torch.zeros(T * (d + 4) + 4, device="cuda")[4:].view(T, d + 4)[:, :d]
+    x.copy_(h)
+    y, _, _ = gaf.gaf_rms_norm(x, w)
+    _, _, want = ref.rms_norm(h, None, w, 1e-6, torch.float32)
+    assert_close(y, want, (ref.RSTD + 2 * ref.U) * want.abs())
