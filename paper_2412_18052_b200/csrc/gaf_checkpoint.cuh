@@ -18,22 +18,24 @@ struct CheckpointArgs {
     void *out;
     unsigned char *codes, *scales;
     int64_t x_stride, codes_stride;
-    int64_t d, tiles_per_row, n_tiles, blocks;
+    int64_t d, blocks;
+    unsigned int tiles_per_row, n_tiles;
 };
 
 template <typename T, bool VEC, bool PACK>
 __global__ void __launch_bounds__(kCheckpointWarps * 32) checkpoint_kernel(const CheckpointArgs a) {
     constexpr int kCheckpointTiles = checkpoint_tiles(VEC);
     const int lane = threadIdx.x & 31;
-    const int64_t first = ((int64_t)blockIdx.x * kCheckpointWarps + (threadIdx.x >> 5)) * kCheckpointTiles;
+    const unsigned int first = (blockIdx.x * kCheckpointWarps + (threadIdx.x >> 5)) * kCheckpointTiles;
     grid_wait();
     if (first >= a.n_tiles) return;
-    int64_t row = first / a.tiles_per_row, tile = first - row * a.tiles_per_row;
+    // (in 32 bits: a 64-bit division was a fifth of the kernel's instructions)
+    unsigned int row = first / a.tiles_per_row, tile = first - row * a.tiles_per_row;
     int64_t rows[kCheckpointTiles], cols[kCheckpointTiles];
 #pragma unroll
     for (int k = 0; k < kCheckpointTiles; ++k) {
         rows[k] = row;
-        cols[k] = tile * kTile;
+        cols[k] = (int64_t)tile * kTile;
         if (++tile == a.tiles_per_row) { tile = 0; ++row; }
     }
     if constexpr (PACK) {

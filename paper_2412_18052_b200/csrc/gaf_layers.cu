@@ -248,7 +248,6 @@ int launch_rms_norm_grad(const NormGradArgs &a, NormFinishArgs f, int dtype, int
 template <bool PACK>
 int launch_checkpoint(const CheckpointArgs &a, int dtype, bool vec, cudaStream_t st) {
     const int64_t ctas = ceil_div(a.n_tiles, int64_t(kCheckpointWarps) * checkpoint_tiles(vec));
-    if (ctas > INT32_MAX) return GAF_ERR_TOO_LARGE;
     return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) {
         return launched(launch_dependent(checkpoint_kernel<typename decltype(t)::type, decltype(v)::value, PACK>, int(ctas), kCheckpointWarps * 32,
                                          st, a), 1);
@@ -439,7 +438,8 @@ int gaf_checkpoint_pack(const void *x, int64_t x_stride, int64_t T, int64_t d, i
     if (i.meets(c) || i.meets(s) || c.meets(s)) return GAF_ERR_ALIAS;
     CheckpointArgs a{};
     a.x = x; a.codes = codes; a.scales = scales; a.x_stride = x_stride; a.codes_stride = codes_stride; a.d = d;
-    a.tiles_per_row = ceil_div(d, kTile); a.n_tiles = T * a.tiles_per_row; a.blocks = blocks_of(d);
+    if (T > INT32_MAX / ceil_div(d, kTile)) return GAF_ERR_TOO_LARGE;      // (tiles are counted in 32 bits)
+    a.tiles_per_row = unsigned(ceil_div(d, kTile)); a.n_tiles = unsigned(T) * a.tiles_per_row; a.blocks = blocks_of(d);
     return launch_checkpoint<true>(a, dtype, wide_rows(d, T, {x_stride}), static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -455,7 +455,8 @@ int gaf_checkpoint_unpack(const uint8_t *codes, int64_t codes_stride, const uint
     CheckpointArgs a{};
     a.out = out; a.codes = const_cast<uint8_t *>(codes); a.scales = const_cast<uint8_t *>(scales);
     a.x_stride = out_stride; a.codes_stride = codes_stride; a.d = d;
-    a.tiles_per_row = ceil_div(d, kTile); a.n_tiles = T * a.tiles_per_row; a.blocks = blocks_of(d);
+    if (T > INT32_MAX / ceil_div(d, kTile)) return GAF_ERR_TOO_LARGE;      // (tiles are counted in 32 bits)
+    a.tiles_per_row = unsigned(ceil_div(d, kTile)); a.n_tiles = unsigned(T) * a.tiles_per_row; a.blocks = blocks_of(d);
     return launch_checkpoint<false>(a, dtype, wide_rows(d, T, {out_stride}), static_cast<cudaStream_t>(cuda_stream));
 }
 
