@@ -684,13 +684,13 @@ const char *gaf_error_string(int code) {
     switch (code) {
         case GAF_OK: return "ok";
         case GAF_ERR_ARG: return "invalid argument";
-        case GAF_ERR_ALIGN: return "device pointer not 16-byte aligned";
-        case GAF_ERR_ALIAS: return "macro_out overlaps an input gradient";
+        case GAF_ERR_ALIGN: return "device pointer not 16-byte aligned (or rows of codes that do not start on 16-byte boundaries)";
+        case GAF_ERR_ALIAS: return "output overlaps an input or another output";
         case GAF_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case GAF_ERR_CUDA: return "CUDA runtime error";
         case GAF_ERR_RESERVED: return "reserved";
         case GAF_ERR_UNSUPPORTED: return "schedule not available for this call on this device";
-        case GAF_ERR_TOO_LARGE: return "size beyond the fixed limit of the no-allocation entry point";
+        case GAF_ERR_TOO_LARGE: return "size beyond the fixed limit of this entry point";
         default: return "unknown error code";
     }
 }

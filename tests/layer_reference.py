@@ -117,7 +117,8 @@ def weight_grad(dy, x, base=None):
     dw = dy.t() @ x
     size = dy.abs().t() @ x.abs()
     # A tensor core adds 16 products to its accumulator at a time, each of the 17 terms cut to 24 bits of the largest: 17 cuts of at most 2 U
-    # of the magnitudes so far, 16 times a chain; then the chains, the splits of the tokens, three terms of dy.
+    # of the magnitudes so far, which are half of the chain's on average, 32 times a chain: 16 * 17 * 2 U; then the chains, the parts of the
+    # tokens, three terms of dy.
     off = (16 * 17 * 2 + dy.shape[0] / 256 * 3 + 300) * U * size
     if base is not None:
         dw = dw + base.to(torch.float64)

@@ -429,9 +429,9 @@ def test_linear_weight_grad_scales_and_special_values():
 
 
 def test_linear_weight_grad_accuracy():
-    """Long sums: no further from binary64 than 1e-6 of the result's norm.  Chains of 16 steps of the tensor core, each of which cuts off up
-    to 2 U of the sum so far, half of that on average: 16 U for a chain whose terms all agree (less for others), then up to 128
-    chains rounded to nearest, whose errors do not add up: under 16 U = 9.6e-7."""
+    """Long sums: no further from binary64 than 1e-6 of the result's norm.  A chain has 32 steps of the tensor core, each of which cuts off up
+    to 2 U of the sum so far, half of that on average, and the sum so far is half of the chain's on average where all terms agree (less for others):
+    16 U for a chain; then up to 64 chains rounded to nearest, whose errors do not add up: under 16 U = 9.6e-7."""
     g = gen(31)
     for T, N, M in ((16384, 256, 256), (8192, 512, 1024)):
         ck, dy = gaf.gaf_checkpoint_pack(randn(g, T, M)), randn(g, T, N, dtype=torch.bfloat16)
