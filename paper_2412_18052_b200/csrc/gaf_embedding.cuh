@@ -239,17 +239,18 @@ __device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned in
     }
 }
 
-// One row of a token that does not occur: base, or zeros.  A warp's work; as 16-byte pieces from the first boundary in the row on, whatever the
-// width (base and gradient lie alike), and single elements before and behind.
+// Rows of tokens that do not occur: base, or zeros.  Neighbouring rows lie next to one another, so that a run of them is one stretch of memory: as
+// 16-byte pieces from its first boundary on, whatever the width (base and gradient lie alike), and single elements before and behind.
 template <typename G>
-__device__ __forceinline__ void fill_row(const EmbedGradArgs &a, int64_t v, int lane) {
+__device__ __forceinline__ void fill_run(const EmbedGradArgs &a, int64_t v, int rows, int lane) {
     constexpr int kBatch = 8, kPer = 16 / sizeof(G);
+    const int64_t n = rows * a.d;
     G *const out = static_cast<G *>(a.grad) + v * a.d;
     const G *const in = static_cast<const G *>(a.base) + v * a.d;
-    const int64_t head = min(a.d, (int64_t)(((16u - (unsigned int)(reinterpret_cast<uintptr_t>(out) & 15u)) & 15u) / sizeof(G)));
-    const int64_t pieces = (a.d - head) / kPer, tail = head + pieces * kPer;
+    const int64_t head = min(n, (int64_t)(((16u - (unsigned int)(reinterpret_cast<uintptr_t>(out) & 15u)) & 15u) / sizeof(G)));
+    const int64_t pieces = (n - head) / kPer, tail = head + pieces * kPer;
     if (lane < head) out[lane] = a.base ? in[lane] : from_float<G>(0.f);
-    if (tail + lane < a.d) out[tail + lane] = a.base ? in[tail + lane] : from_float<G>(0.f);
+    if (tail + lane < n) out[tail + lane] = a.base ? in[tail + lane] : from_float<G>(0.f);
     uint4 *const to = reinterpret_cast<uint4 *>(out + head);
     const uint4 *const from = reinterpret_cast<const uint4 *>(in + head);
     for (int64_t c0 = lane; c0 < pieces; c0 += 32 * kBatch) {
@@ -259,6 +260,18 @@ __device__ __forceinline__ void fill_row(const EmbedGradArgs &a, int64_t v, int 
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
             if (c0 + 32 * k < pieces) to[c0 + 32 * k] = x[k];
+    }
+}
+// Rows that a warp looks at together: enough of them for some KB.  And the runs among those of them (bits of `absent`) that do not occur.
+template <typename G>
+__device__ __forceinline__ int fill_group(int64_t d) { return d * (int64_t)sizeof(G) >= 1024 ? 8 : 32; }
+template <typename G>
+__device__ __forceinline__ void fill_absent(const EmbedGradArgs &a, int64_t v0, unsigned int absent, int lane) {
+    while (absent != 0u) {
+        const int first = __ffs(absent) - 1, past = __ffs(~(absent >> first)) - 1;      // (-1: ones to the end)
+        const int rows = past < 0 ? 32 - first : past;
+        fill_run<G>(a, v0 + first, rows, lane);
+        absent &= first + rows >= 32 ? 0u : ~0u << (first + rows);
     }
 }
 // The first half of the rows is filled beside the grouping, the other half beside the sums.
@@ -278,8 +291,11 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs &a, unsigned int *
             if (v >= 0 && v < to - from) atomicOr(bits + (v >> 5), 1u << (v & 31));
         }
         __syncthreads();
-        for (int64_t v = from + warp; v < to; v += kGroupThreads / 32)
-            if (((bits[(v - from) >> 5] >> ((v - from) & 31)) & 1u) == 0u) fill_row<G>(a, v, lane);
+        const int group = fill_group<G>(a.d);
+        for (int64_t v = from + warp * group; v < to; v += kGroupThreads / 32 * group) {
+            const int rows = (int)min((int64_t)group, to - v);
+            fill_absent<G>(a, v, ~(bits[(v - from) >> 5] >> ((v - from) & 31)) & (0xFFFFFFFFu >> (32 - rows)), lane);
+        }
         __syncthreads();
     }
 }
@@ -343,15 +359,16 @@ __global__ void __launch_bounds__(kEmbedWarps * 32, 2) embedding_sum_kernel(cons
     const int role = blockIdx.x % 3, summing = 3 - a.fillers;
     if (role >= summing) {
         if (a.base == a.grad) return;
-        const int64_t stride = (int64_t)(gridDim.x / 3) * a.fillers * kEmbedWarps * 8;
-        // a warp looks at 8 counts at a time, and fetches the next ones before it writes
-        auto counts = [&](int64_t v0) { return lane < 8 && v0 + lane < a.V ? a.count[v0 + lane] : 1u; };
-        int64_t v0 = fill_split(a.V) + ((int64_t)((blockIdx.x / 3) * a.fillers + role - summing) * kEmbedWarps + (threadIdx.x >> 5)) * 8;
+        const int group = fill_group<G>(a.d);
+        const int64_t stride = (int64_t)(gridDim.x / 3) * a.fillers * kEmbedWarps * group;
+        // (the next counts are fetched before these rows are written)
+        auto counts = [&](int64_t v0) { return lane < group && v0 + lane < a.V ? a.count[v0 + lane] : 1u; };
+        int64_t v0 = fill_split(a.V) + ((int64_t)((blockIdx.x / 3) * a.fillers + role - summing) * kEmbedWarps + (threadIdx.x >> 5)) * group;
         unsigned int n = counts(v0);
         for (; v0 < a.V; v0 += stride) {
             const unsigned int absent = __ballot_sync(0xFFFFFFFFu, n == 0u);
             n = counts(v0 + stride);
-            for (unsigned int m = absent; m != 0u; m &= m - 1u) fill_row<G>(a, v0 + __ffs(m) - 1, lane);
+            fill_absent<G>(a, v0, absent, lane);
         }
         return;
     }

@@ -697,3 +697,25 @@ def test_dense_neighbours_of_every_alignment():
     y, _, _ = gaf.gaf_rms_norm(x, w)
     _, _, want = ref.rms_norm(h, None, w, 1e-6, torch.float32)
     assert_close(y, want, (ref.RSTD + 2 * ref.U) * want.abs())
+
+
+@pytest.mark.parametrize("grad_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,d", [(5000, 1), (3001, 3), (4096, 7), (2050, 33), (1000, 64), (999, 250), (700, 257), (515, 1030)])
+def test_embedding_grad_of_rows_that_do_not_occur(V, d, grad_dtype):
+    """Runs of absent rows of every length, at every alignment: zeros, or base, and nothing else."""
+    g, gt = gen(V + d), TYPES[grad_dtype]
+    T = 60
+    dy = randn(g, T, d, dtype=torch.bfloat16)
+    tokens = torch.randint(0, V, (T,), generator=g, device="cuda")
+    tokens[:8] = torch.tensor([0, 1, 31, 32, 33, V // 2, V // 2 - 1, V - 1], device="cuda")
+    ws = workspace(T, d, torch.bfloat16, V=V)
+    for base in (None, randn(g, V, d, dtype=gt)):
+        place = Slice((V, d), gt)
+        place.view.fill_(float("nan"))
+        gaf.gaf_embedding_grad(dy, tokens, place.view, ws, base=base)
+        absent = torch.ones(V, dtype=torch.bool, device="cuda")
+        absent[tokens] = False
+        want = torch.zeros(V, d, dtype=gt, device="cuda") if base is None else base
+        assert torch.equal(place.view[absent], want[absent])
+        assert_close(place.view, *ref.embedding_grad(dy, tokens, V, 1.0, base))
+        place.check_guards()
