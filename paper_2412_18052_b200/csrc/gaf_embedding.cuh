@@ -12,7 +12,7 @@
 //            stretch differs from run to run; stretches of more than 32 are therefore put in ascending order here (a warp each, a
 //            bit per position), shorter ones by the warp that adds them.  All other CTAs meanwhile write the rows of tokens that do
 //            not occur, of the first half of the table, each after looking through the tokens for those of its own range.  (Grouping first, then one
-//            kernel that met every row and looked up its count: 67.6 and 479 us where this takes 35 and 324, at 1000
+//            kernel that met every row and looked up its count: 67.6 and 479 us where this takes 36 and 328, at 1000
 //            tokens, 50,257 x 768 binary32, and 32,768 tokens, 100,000 x 2048 with a base.)
 //   sum + fill   Beside what is left to fill (half of the rows: the sums are bound by latency, the filling by bandwidth), a warp per occurring token
 //            and 256 columns adds its positions in ascending order in binary32 registers.  Stretches of

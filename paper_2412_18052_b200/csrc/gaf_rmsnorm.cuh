@@ -3,7 +3,7 @@
 //     h = x + residual (rounded to the matrices' type)      r = 1 / sqrt(mean h^2 + eps)      y = h r w
 //     dx = residual_grad + r (w dy - h r^2 mean(w dy h))     dw = sum over rows of dy h r
 //
-// Both are bound by memory (16384 x 4096 bfloat16: forward with residual and coded result 99 us, 6.1 TB/s; backward from an 8-bit checkpoint with a
+// Both are bound by memory (16384 x 4096 bfloat16: forward with residual and coded result 97 us, 6.2 TB/s; backward from an 8-bit checkpoint with a
 // residual's gradient 90 us, 5.2 TB/s, issue slots half taken).  A row is held in registers between its reduction and its results, so that everything is read and
 // written once: R threads of a CTA share a row, up to S tiles of 256 columns per warp.
 #pragma once

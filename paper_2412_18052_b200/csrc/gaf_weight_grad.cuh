@@ -13,7 +13,7 @@
 // 1024 clocks of the tensor core, an SM's shared memory takes in 48 KB of copies, is read for 16 KB and written 32 KB by widening, and read for
 // 64 KB by the MMAs: 160 of the 128 bytes a clock that it has, so that the tensor cores cannot be busy for more than four fifths of the time.
 //
-// Measured at T = 16384, N = M = 4096, dW in binary32: 500 us with random data (1.10 PFLOP/s, 0.66 of the measured cuBLAS burst, 0.78 of
+// Measured at T = 16384, N = M = 4096, dW in binary32: 495 us with random data (1.11 PFLOP/s, 0.66 of the measured cuBLAS burst, 0.79 of
 // its rate under the power limit), 425 us in short runs; tensor pipe active 71 % of the
 // cycles.  T = 300, N = M = 768: 10.7 us, two launches.
 //
