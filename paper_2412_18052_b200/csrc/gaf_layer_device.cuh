@@ -23,10 +23,6 @@ constexpr int kTile = 256;
 template <bool VEC>
 __device__ __forceinline__ int tile_column(int lane, int i) { return VEC ? lane * 8 + i : i * 32 + lane; }
 
-// Whether a lane's element i lies in a row of which `left` columns remain from the tile's first one on.
-template <bool VEC>
-__device__ __forceinline__ bool tile_has(int lane, int i, int64_t left) { return tile_column<VEC>(lane, i) < left; }
-
 __device__ __forceinline__ void unpack_bf16x8(const uint4 &r, float (&v)[8]) {
     const unsigned int w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll

@@ -13,8 +13,8 @@
 // 1024 clocks of the tensor core, an SM's shared memory takes in 48 KB of copies, is read for 16 KB and written 32 KB by widening, and read for
 // 64 KB by the MMAs: 160 of the 128 bytes a clock that it has, so that the tensor cores cannot be busy for more than four fifths of the time.
 //
-// Measured at T = 16384, N = M = 4096, dW in binary32: 495 us with random data (1.11 PFLOP/s, 0.66 of the measured cuBLAS burst, 0.79 of
-// its rate under the power limit), 425 us in short runs; tensor pipe active 71 % of the
+// Measured at T = 16384, N = M = 4096, dW in binary32: 480 us with random data (1.14 PFLOP/s, 0.68 of the measured cuBLAS burst, 0.82 of
+// its rate under the power limit), 421 us in short runs; tensor pipe active 71 % of the
 // cycles.  T = 300, N = M = 768: 10.7 us, two launches.
 //
 // Accuracy.  A tensor core adds to its binary32 accumulator by cutting off, not by rounding; over many steps that pulls a sum
@@ -48,7 +48,6 @@ constexpr int kWgChunk = 512;                           // tokens per chain
 constexpr int kWgChunkSteps = kWgChunk / kWgK;
 constexpr int kWgDyBytes = kWgK * (kWgN / 2) * 2, kWgCodeBytes = kWgK * kWgM, kWgWideBytes = kWgK * kWgM * 2;
 constexpr int kWgSmem = kWgRing * (kWgDyBytes + kWgWideBytes) + kWgCodeRing * kWgCodeBytes + 1024;
-constexpr int kWgGroups = 1;                            // groups of the widening warps, which take steps in turn
 constexpr uint32_t kWgScalesAhead = 1;                  // steps whose scales are in flight (less than the ring holds)
 constexpr int kWgThreads = 640;
 constexpr int kWgNapEpilogue = 400, kWgNapWiden = 0, kWgNapCopy = 100, kWgNapMma = 0;
@@ -260,11 +259,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         for (int s = 0; s < kWgCodeRing; ++s) {
             // codes, scales
             tc_mbar_init(&sh.code_full[s], 2 + (s == 0 && a.test_extra_arrival ? 1 : 0));
-            tc_mbar_init(&sh.code_empty[s], 8 / kWgGroups);
+            tc_mbar_init(&sh.code_empty[s], 8);          // the widening warps
         }
         for (int s = 0; s < kWgRing; ++s) {
             tc_mbar_init(&sh.dy_full[s], 1);
-            tc_mbar_init(&sh.wide_full[s], 8 / kWgGroups);   // a group's warps
+            tc_mbar_init(&sh.wide_full[s], 8);
             tc_mbar_init(&sh.done[s], 1);
             tc_mbar_init(&sh.other[s], 1);
         }
@@ -289,11 +288,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     grid_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
 
-    // 5 x 128 threads with 96 registers each: 2 x 168 + 2 x 48 + 48 = 480 (nothing spills: what a thread stores to local memory, its
+    // 5 x 128 threads with 96 registers each: 2 x 160 + 2 x 48 + 64 = 480 (nothing spills: what a thread stores to local memory, its
     // fence for the tensor cores would wait for)
     if (warp < 8) {
         // ------------------------------------------------------------ epilogue ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
         uint32_t chain = 0;
@@ -338,23 +337,21 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     } else if (warp < 16) {
         // ------------------------------------------------------------ widening ----
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        constexpr int kRows = 8 * (8 / kWgGroups), kUnits = kWgK / kRows;       // rows of a group at a time
-        const int group = (warp - 8) / (8 / kWgGroups);
+        constexpr int kRows = 64, kUnits = kWgK / kRows;         // rows of the warps at a time
         // A unit is 16 codes of a row.  Four lanes take the four units of half a row (64 codes, one swizzle atom of the widened step), the four
         // lanes next to them those of the row whose number differs by 5: then neither the codes (swizzled by the copy) nor what is written
         // meets another lane's banks.  A warp takes 8 rows at a time.
-        const int j = lane & 3, pair_of = lane >> 3, row = ((pair_of & 3) ^ ((lane & 4) ? 5 : 0)) + (warp - 8) % (8 / kWgGroups) * 8;
+        const int j = lane & 3, pair_of = lane >> 3, row = ((pair_of & 3) ^ ((lane & 4) ? 5 : 0)) + (warp - 8) * 8;
         const uint32_t code_at = (uint32_t)(row * kWgM + ((j ^ (row & 7)) << 4));                   // first half of the row; the second: ^ 64
         const uint32_t at0 = (uint32_t)(row * 128 + ((2 * j) ^ (row & 7)) * 16), at1 = (uint32_t)(row * 128 + ((2 * j + 1) ^ (row & 7)) * 16);
-        int s = group, o = group, skip = group;          // skip: steps of the other groups before the next one of this
+        int s = 0, o = 0;
         uint32_t full_phase = 0, wide_phase = 1;         // (the first round finds every widened step's place free)
         bool alive = true;
         for (int item = pair; item < a.items && alive; item += pairs) {
             const WgItem w = wg_item(a, item, rank);
             // (a multiple of 4 tokens further on, a scale byte lies at the same place of its word)
             const int shift = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
-            int step = w.step0 + skip;
-            for (; step < w.step1; step += kWgGroups) {
+            for (int step = w.step0; step < w.step1; ++step) {
                 // (two lanes poll the codes' barrier and that of the place they go to)
                 if (!wg_wait_warp<kWgNapWiden>(lane == 0 ? &sh.code_full[s] : &sh.done[o], lane == 0 ? full_phase : wide_phase, &sh.abort_flag,
                                                a.spin_limit)) { alive = false; break; }
@@ -393,13 +390,12 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 }
                 __syncwarp();
                 wg_arrive_warp(&sh.wide_full[o]);
-                if ((s += kWgGroups) >= kWgCodeRing) { s -= kWgCodeRing; full_phase ^= 1u; }
-                if ((o += kWgGroups) >= kWgRing) { o -= kWgRing; wide_phase ^= 1u; }
+                if (++s == kWgCodeRing) { s = 0; full_phase ^= 1u; }
+                if (++o == kWgRing) { o = 0; wide_phase ^= 1u; }
             }
-            skip = step - w.step1;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 16) {
             // ------------------------------------------------- copies of dy ----
             if (lane == 0) {
@@ -420,7 +416,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 }
                 // what is in flight lands before the CTA ends, also after a wait gave up
                 for (uint32_t i = issued > kWgRing ? issued - kWgRing : 0; i < issued; ++i)
-                    for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
+                    for (unsigned int spin = 0; spin < min(a.spin_limit, kTcSpinLimit); ++spin)
                         if (tc_mbar_try(&sh.dy_full[i % kWgRing], (i / kWgRing) & 1u, 2000u)) break;
             }
             __syncwarp();
@@ -466,7 +462,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 // tensor memory is not freed, and no shared memory left, under MMAs in flight
                 if (wg_elected()) {
                     wg_commit_own(&sh.drained);
-                    for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
+                    for (unsigned int spin = 0; spin < min(a.spin_limit, kTcSpinLimit); ++spin)
                         if (tc_mbar_try(&sh.drained, 0u, 2000u)) break;
                 }
                 __syncwarp();
@@ -502,7 +498,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     }
                 }
                 for (uint32_t i = issued > kWgCodeRing ? issued - kWgCodeRing : 0; i < issued; ++i)
-                    for (unsigned int spin = 0; spin < a.spin_limit; ++spin)
+                    for (unsigned int spin = 0; spin < min(a.spin_limit, kTcSpinLimit); ++spin)
                         if (tc_mbar_try(&sh.code_full[i % kWgCodeRing], (i / kWgCodeRing) & 1u, 2000u)) break;
             }
             __syncwarp();
