@@ -330,7 +330,8 @@ int gaf_pairwise_cosdist(const void *const *grads, int K, int64_t D, int dtype,
                          void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
- * Read the device status word of the most recent call that used `workspace`.
+ * Read the device status of `workspace`: that of the most recent filter call (of a streaming filter, of all its pushes), and
+ * GAF_STATUS_TIMEOUT if a wait of the most recent gaf_linear_weight_grad ran out.
  * SYNCHRONISES the stream.  *status_out receives GAF_STATUS_* bits.
  */
 int gaf_read_status(const void *workspace, void *cuda_stream, int *status_out);
@@ -393,7 +394,7 @@ int gaf_cosdist_static(const void *x, const void *y, int64_t D, int dtype,
  *   - Outputs must not overlap inputs or one another (GAF_ERR_ALIAS) except as said.
  *   - Infinities and NaN go through the arithmetic; nothing is screened.
  *   - `workspace`: gaf_layer_workspace_bytes; its contents do not matter, before or between calls.  It may be the
- *     filter's workspace (prepared by gaf_workspace_init) if that is large enough: the layers leave alone what the filter keeps there.  Calls that share
+ *     filter's workspace (prepared by gaf_workspace_init) if that is large enough: the layers leave alone what the filter keeps there, its status included.  Calls that share
  *     one are ordered on one stream; graphs that are replayed at the same time need one each.
  *     gaf_read_status tells whether a bounded wait of gaf_linear_weight_grad ran out (GAF_STATUS_TIMEOUT).
  */

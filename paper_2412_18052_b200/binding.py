@@ -339,7 +339,8 @@ def gaf_linear_weight_grad(dy: torch.Tensor, checkpoint: Checkpoint, dweight: to
 
 
 def gaf_read_status(workspace: torch.Tensor) -> int:
-    """Status bits of the latest call on this workspace (synchronises the stream)."""
+    """Status bits of the latest filter call on this workspace, and GAF_STATUS_TIMEOUT if the latest weight gradient's wait ran out (synchronises
+    the stream)."""
     out = ctypes.c_int()
     _check(lib().gaf_read_status(workspace.data_ptr(), _stream(), ctypes.byref(out)), "gaf_read_status")
     return out.value

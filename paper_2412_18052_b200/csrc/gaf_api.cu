@@ -1099,10 +1099,15 @@ int gaf_read_status(const void *workspace, void *cuda_stream, int *status_out) {
     if (!workspace || !status_out) return GAF_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Control *ctl = static_cast<const Control *>(workspace);
-    int status = 0;
-    if (cudaMemcpyAsync(&status, &ctl->status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess)
+    int words[2] = {0, 0};              // the filter's and the layers'
+    static_assert(offsetof(Control, layer_status) == offsetof(Control, status) + sizeof(int), "read together");
+    if (cudaMemcpyAsync(words, &ctl->status, sizeof(words), cudaMemcpyDeviceToHost, st) != cudaSuccess)
         return GAF_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return GAF_ERR_CUDA;
+    // (other bits: memory that only layers have used, and that was not prepared)
+    constexpr int kKnown = GAF_STATUS_ZERO_NORM | GAF_STATUS_NONFINITE | GAF_STATUS_TIMEOUT | GAF_STATUS_ILL_CONDITIONED;
+    int status = (words[0] & ~kKnown) == 0 ? words[0] : 0;
+    if (static_cast<unsigned int>(words[1]) == kLayerTimeout) status |= GAF_STATUS_TIMEOUT;
     *status_out = status;
     return GAF_OK;
 }

@@ -20,7 +20,8 @@ struct Control {
     unsigned int pair_hint;             // one-launch schedule with two gradients: what the latest two calls kept (0 both, 1 the seed alone, 2 | latest: they differed)
     unsigned int reserved1;
     int mean_done;                      // two-launch form: 1 = the first launch has written the result
-    int status;                         // GAF_STATUS_* bits of the latest call
+    int status;                         // GAF_STATUS_* bits of the latest filter call
+    unsigned int layer_status;          // kLayerTimeout: a bounded wait of the layers' latest weight gradient ran out; anything else: none did
     int count;                          // running c of Algorithm 1
     int ring_seed;                      // any-seed variant: the winning seed, else -1
     unsigned long long accept_bits;     // Gram-first schedule: bit t set = step t accepted
@@ -31,6 +32,7 @@ struct Control {
     double norm_sq_sum;                 // stepwise and streaming forms: sum of |g_i|^2 over the accepted gradients
     unsigned int two_launch_calls;      // calls of the two-launch form of gaf_fused.cuh so far: the next one's tag is one more
 };
+constexpr unsigned int kLayerTimeout = 0x74696D65u;     // (a word of memory that was never prepared is hardly this)
 constexpr size_t kControlBytes = 4096;  // sizeof(Control) rounded up
 static_assert(sizeof(Control) <= kControlBytes, "control block");
 // After the control block: double partials[kMaxCtas][3], then operation-specific space.

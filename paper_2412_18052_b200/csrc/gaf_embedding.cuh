@@ -85,7 +85,6 @@ struct GroupCursors { unsigned int lights, positions, pieces, heavies; };      /
 struct EmbedGradArgs {
     const void *dy, *tokens, *base;
     void *grad;
-    Control *ctl;
     GroupCursors *cur;
     unsigned int *count;        // [V] positions of a token
     unsigned int *start;        // [V] first place of its stretch
@@ -123,10 +122,7 @@ __device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned in
     const int64_t tid = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x;
     const int lane = threadIdx.x & 31;
     for (int64_t v = tid; v < a.V; v += kThreads) a.count[v] = 0u;
-    if (tid == 0) {
-        *a.cur = GroupCursors{0u, 0u, 0u, 0u};
-        a.ctl->status = 0;
-    }
+    if (tid == 0) *a.cur = GroupCursors{0u, 0u, 0u, 0u};
     cluster_barrier();
     // counts; lanes with the same token take their places together
     for (int64_t t0 = tid - lane; t0 < a.T; t0 += kThreads) {

@@ -335,7 +335,6 @@ int gaf_embedding_grad(const void *dy, int64_t dy_stride, int64_t T, int64_t d, 
     if (!device_info(&di)) return GAF_ERR_CUDA;
     EmbedGradArgs a{};
     a.dy = dy; a.tokens = tokens; a.base = base; a.grad = grad;
-    a.ctl = static_cast<Control *>(workspace);
     a.cur = in_workspace<GroupCursors>(workspace, l.cursors);
     a.count = in_workspace<unsigned int>(workspace, l.count);
     a.start = in_workspace<unsigned int>(workspace, l.start);
@@ -418,7 +417,6 @@ int gaf_rms_norm_grad(const void *dy, int64_t dy_stride, const void *h, int64_t 
     NormGradArgs a{};
     a.dy = dy; a.h = h; a.weight = weight; a.residual_grad = residual_grad; a.h_codes = h_codes; a.h_scales = h_scales; a.rstd = rstd; a.dx = dx;
     a.partials = in_workspace<float>(workspace, kLayerScratchOffset);
-    a.ctl = static_cast<Control *>(workspace);
     a.dy_stride = dy_stride; a.h_stride = h_stride; a.codes_stride = h_codes_stride; a.residual_grad_stride = residual_grad_stride;
     a.T = T; a.d = d; a.blocks = blocks_of(d);
     NormFinishArgs f{};

@@ -108,7 +108,6 @@ struct NormGradArgs {
     const float *rstd;
     void *dx;
     float *partials;            // [CTA][d]: sums over the CTA's rows
-    Control *ctl;
     int64_t dy_stride, h_stride, codes_stride, residual_grad_stride;
     int64_t T, d, blocks;
 };
@@ -143,7 +142,6 @@ __global__ void __launch_bounds__(norm_threads(R)) rms_norm_grad_kernel(const No
         r = row < a.T ? a.rstd[row] : 0.f;
     };
     grid_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t row = (int64_t)blockIdx.x * kRows + sub;
 #pragma unroll

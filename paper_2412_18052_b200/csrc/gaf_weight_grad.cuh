@@ -286,7 +286,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
     grid_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->status = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->layer_status = 0u;
 
     // 5 x 128 threads with 96 registers each: 2 x 160 + 2 x 48 + 64 = 480 (nothing spills: what a thread stores to local memory, its
     // fence for the tensor cores would wait for)
@@ -550,7 +550,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     tc_fence_after_sync();
     if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kWgTmemCols) : "memory");
-    if (sh.abort_flag && threadIdx.x == 0) atomicOr(&a.ctl->status, kStatusTimeoutBit);
+    if (sh.abort_flag && threadIdx.x == 0) a.ctl->layer_status = kLayerTimeout;
 }
 
 // dW = base + the parts' sums in order, of the tiles whose tokens were split.  Four elements of a row per thread.

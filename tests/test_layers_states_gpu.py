@@ -1,0 +1,69 @@
+"""What the layers' calls leave for later calls to find, and what they do at the edges of their arguments."""
+import pytest
+import torch
+
+import paper_2412_18052_b200 as gaf
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape, dtype=torch.float32, size=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * size).to(dtype)
+
+
+class Layers:
+    """One call of each of the gradients on a workspace."""
+    T, d, V = 200, 264, 300
+
+    def __init__(self, seed=1):
+        g = gen(seed)
+        self.dy, self.h, self.w = randn(g, self.T, self.d), randn(g, self.T, self.d), randn(g, self.d)
+        self.rstd, self.ck = torch.ones(self.T, device="cuda"), gaf.gaf_checkpoint_pack(self.h)
+        self.tokens = torch.randint(0, self.V, (self.T,), generator=g, device="cuda")
+
+    def bytes(self):
+        return gaf.gaf_layer_workspace_bytes(self.T, self.d, gaf.GAF_F32, self.V)
+
+    def embedding(self, ws):
+        return gaf.gaf_embedding_grad(self.dy, self.tokens, torch.empty(self.V, self.d, device="cuda"), ws)
+
+    def norm(self, ws):
+        return gaf.gaf_rms_norm_grad(self.dy, self.h, self.w, self.rstd, torch.empty(self.d, device="cuda"), ws)
+
+    def linear(self, ws):
+        return gaf.gaf_linear_weight_grad(self.dy, self.ck, torch.empty(self.d, self.d, device="cuda"), ws)
+
+    def calls(self):
+        return [self.embedding, self.norm, self.linear]
+
+
+# ------------------------------------------------------------------ status ----
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_layers_between_the_arrivals_of_a_stream(which):
+    """A filter that takes its gradients one at a time, the layers making the next one in between on the same workspace: what an arrival left
+    in the status is still there at the end, and decisions and distances are those of a workspace of its own."""
+    L, D = Layers(), 4096
+    n = max(L.bytes(), gaf.gaf_workspace_bytes(4, D, gaf.GAF_F32))
+    shared, alone = torch.empty(n, dtype=torch.uint8, device="cuda"), gaf.new_workspace(4, D, gaf.GAF_F32)
+    gaf.gaf_workspace_init(shared)
+    for bad, bit in ((0.0, gaf.GAF_STATUS_ZERO_NORM), (float("nan"), gaf.GAF_STATUS_NONFINITE)):
+        grads = [randn(gen(k), D) for k in range(4)]
+        grads[1].fill_(bad)
+        got = []
+        for ws, between in ((shared, True), (alone, False)):
+            acc = torch.empty(D, device="cuda")
+            gaf.gaf_stream_begin(grads[0], acc, ws)
+            for t in (1, 2, 3):
+                gaf.gaf_stream_push(grads[t], t, 0.97, acc, ws)
+                if between:
+                    L.calls()[which](ws)
+            got.append((acc, *gaf.gaf_stream_end(4, acc, ws)))
+            assert gaf.gaf_read_status(ws) & bit, between
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(*got))      # (bits: a distance may be NaN)
