@@ -331,7 +331,8 @@ int gaf_pairwise_cosdist(const void *const *grads, int K, int64_t D, int dtype,
 
 /*
  * Read the device status of `workspace`: that of the most recent filter call (of a streaming filter, of all its pushes), and
- * GAF_STATUS_TIMEOUT if a wait of the most recent gaf_linear_weight_grad ran out.
+ * GAF_STATUS_TIMEOUT if a wait of any gaf_linear_weight_grad has run out since the status was last read (reading tells it once) or
+ * gaf_workspace_init: a microbatch is checked once, at its end.
  * SYNCHRONISES the stream.  *status_out receives GAF_STATUS_* bits.
  */
 int gaf_read_status(const void *workspace, void *cuda_stream, int *status_out);
@@ -393,10 +394,12 @@ int gaf_cosdist_static(const void *x, const void *y, int64_t D, int dtype,
  *     weight that is used twice (an embedding table that is the output layer's weight too).  It may be the output itself.
  *   - Outputs must not overlap inputs or one another (GAF_ERR_ALIAS) except as said.
  *   - Infinities and NaN go through the arithmetic; nothing is screened.
- *   - `workspace`: gaf_layer_workspace_bytes; its contents do not matter, before or between calls.  It may be the
+ *   - `workspace`: gaf_layer_workspace_bytes; its contents do not matter to any result, before or between calls (gaf_read_status
+ *     expects that gaf_workspace_init was called once: memory may hold an older workspace's status).  It may be the
  *     filter's workspace (prepared by gaf_workspace_init) if that is large enough: the layers leave alone what the filter keeps there, its status included.  Calls that share
  *     one are ordered on one stream; graphs that are replayed at the same time need one each.
- *     gaf_read_status tells whether a bounded wait of gaf_linear_weight_grad ran out (GAF_STATUS_TIMEOUT).
+ *     gaf_read_status tells whether a bounded wait of gaf_linear_weight_grad ran out (GAF_STATUS_TIMEOUT): that call's gradient, and what was made of
+ *     it, is not valid.  No call clears that, only reading it does.
  */
 
 /*

@@ -271,9 +271,11 @@ def gaf_layer_workspace_bytes(T: int, width: int, dtype: int, V: int = 0) -> int
 
 def new_layer_workspace(T: int, width: int, dtype: int, V: int = 0, device=None) -> torch.Tensor:
     """Workspace of the layers' gradients for up to T tokens, matrices of up to ``width`` columns and tables of V rows
-    (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter (but to the filter: a workspace that
-    is to serve both goes through gaf_workspace_init once)."""
-    return torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
+    (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter to any result; it is prepared by
+    gaf_workspace_init all the same, for its status and for the filter, which it serves too if it is large enough."""
+    ws = torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
+    gaf_workspace_init(ws)
+    return ws
 
 
 Checkpoint = Tuple[torch.Tensor, torch.Tensor]
@@ -339,8 +341,8 @@ def gaf_linear_weight_grad(dy: torch.Tensor, checkpoint: Checkpoint, dweight: to
 
 
 def gaf_read_status(workspace: torch.Tensor) -> int:
-    """Status bits of the latest filter call on this workspace, and GAF_STATUS_TIMEOUT if the latest weight gradient's wait ran out (synchronises
-    the stream)."""
+    """Status bits of the latest filter call on this workspace, and GAF_STATUS_TIMEOUT if a wait of any weight gradient has run out since the
+    status was last read (synchronises the stream)."""
     out = ctypes.c_int()
     _check(lib().gaf_read_status(workspace.data_ptr(), _stream(), ctypes.byref(out)), "gaf_read_status")
     return out.value

@@ -1107,7 +1107,10 @@ int gaf_read_status(const void *workspace, void *cuda_stream, int *status_out) {
     // (other bits: memory that only layers have used, and that was not prepared)
     constexpr int kKnown = GAF_STATUS_ZERO_NORM | GAF_STATUS_NONFINITE | GAF_STATUS_TIMEOUT | GAF_STATUS_ILL_CONDITIONED;
     int status = (words[0] & ~kKnown) == 0 ? words[0] : 0;
-    if (static_cast<unsigned int>(words[1]) == kLayerTimeout) status |= GAF_STATUS_TIMEOUT;
+    if (static_cast<unsigned int>(words[1]) == kLayerTimeout) {
+        status |= GAF_STATUS_TIMEOUT;           // told once
+        if (cudaMemsetAsync(const_cast<unsigned int *>(&ctl->layer_status), 0, sizeof(ctl->layer_status), st) != cudaSuccess) return GAF_ERR_CUDA;
+    }
     *status_out = status;
     return GAF_OK;
 }

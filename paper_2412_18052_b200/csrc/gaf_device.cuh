@@ -21,7 +21,7 @@ struct Control {
     unsigned int reserved1;
     int mean_done;                      // two-launch form: 1 = the first launch has written the result
     int status;                         // GAF_STATUS_* bits of the latest filter call
-    unsigned int layer_status;          // kLayerTimeout: a bounded wait of the layers' latest weight gradient ran out; anything else: none did
+    unsigned int layer_status;          // kLayerTimeout: a bounded wait of a weight gradient has run out since the status was last read; anything else: none
     int count;                          // running c of Algorithm 1
     int ring_seed;                      // any-seed variant: the winning seed, else -1
     unsigned long long accept_bits;     // Gram-first schedule: bit t set = step t accepted

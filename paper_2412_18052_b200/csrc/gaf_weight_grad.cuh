@@ -286,7 +286,6 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
     grid_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.ctl->layer_status = 0u;
 
     // 5 x 128 threads with 96 registers each: 2 x 160 + 2 x 48 + 64 = 480 (nothing spills: what a thread stores to local memory, its
     // fence for the tensor cores would wait for)

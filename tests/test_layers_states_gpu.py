@@ -67,3 +67,37 @@ def test_layers_between_the_arrivals_of_a_stream(which):
             got.append((acc, *gaf.gaf_stream_end(4, acc, ws)))
             assert gaf.gaf_read_status(ws) & bit, between
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(*got))      # (bits: a distance may be NaN)
+
+
+def test_a_wait_that_ran_out_is_told_after_later_calls():
+    """GAF_STATUS_TIMEOUT of a weight gradient stays, through the calls that follow it on the workspace, until it has been read."""
+    L, D = Layers(), 4096
+    n = max(L.bytes(), gaf.gaf_workspace_bytes(2, D, gaf.GAF_F32))
+    grads = [randn(gen(k), D) for k in range(2)]
+    for after in (L.calls(), [L.linear], [L.norm], [L.embedding], [lambda ws: gaf.gaf_filter_accumulate(grads, 2.0, ws)]):
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        gaf.gaf_workspace_init(ws)
+        gaf.gaf_test_set_wait_fault(50, 1)
+        try:
+            L.linear(ws)
+        finally:
+            gaf.gaf_test_set_wait_fault(0, False)
+        for call in after:
+            call(ws)
+        assert gaf.gaf_read_status(ws) == gaf.GAF_STATUS_TIMEOUT
+        assert gaf.gaf_read_status(ws) == 0                      # (told once)
+        for call in after:
+            call(ws)
+        assert gaf.gaf_read_status(ws) == 0
+
+
+@pytest.mark.parametrize("fill", [0, 1, 4, 15, 0x4D4D4D4D, -1])
+def test_status_of_a_workspace_that_held_anything(fill):
+    """A workspace for the layers alone says nothing of what the memory held before."""
+    L = Layers()
+    old = torch.full((L.bytes() // 4,), fill, dtype=torch.int32, device="cuda")
+    del old                                                      # (the allocator hands the same memory out again)
+    ws = gaf.new_layer_workspace(L.T, L.d, gaf.GAF_F32, V=L.V)
+    for call in L.calls():
+        call(ws)
+    assert gaf.gaf_read_status(ws) == 0
