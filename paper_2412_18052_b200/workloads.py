@@ -255,6 +255,7 @@ class LanguageModel:
 
 def language_model(K: int, V: int, d: int, T: int, seed: int = 0, dtype: str = "f32", taus: Sequence[float] = (0.97,)) -> Workload:
     """K micro-gradients of a ``LanguageModel`` on microbatches of T tokens, made on the GPU by the library's layers."""
+    from . import binding
     model = LanguageModel(V, d, seed)
     w = Workload("language_model", K, model.D, dtype, [float(t) for t in taus], [], seed)
     workspace, tdtype = model.new_workspace(T), torch.float32 if dtype == "f32" else torch.bfloat16
@@ -263,4 +264,6 @@ def language_model(K: int, V: int, d: int, T: int, seed: int = 0, dtype: str = "
         tokens = model.tokens(T, seed * 1000 + 2 * k)
         model.micro_gradient(tokens, model.tokens(T, seed * 1000 + 2 * k + 1).clamp(min=0), flat, workspace)
         w.grads.append(flat)
+    if binding.gaf_read_status(workspace) & binding.GAF_STATUS_TIMEOUT:
+        raise RuntimeError("a bounded wait of a weight gradient ran out: the micro-gradients are not valid")
     return w

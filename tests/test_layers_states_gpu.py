@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2412_18052_b200 as gaf
+from paper_2412_18052_b200 import workloads
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +102,13 @@ def test_status_of_a_workspace_that_held_anything(fill):
     for call in L.calls():
         call(ws)
     assert gaf.gaf_read_status(ws) == 0
+
+
+def test_workload_with_a_wait_that_ran_out_is_refused():
+    gaf.gaf_test_set_wait_fault(50, 1)
+    try:
+        with pytest.raises(RuntimeError, match="ran out"):
+            workloads.language_model(2, 300, 128, 100)
+    finally:
+        gaf.gaf_test_set_wait_fault(0, False)
+    assert len(workloads.language_model(2, 300, 128, 100).grads) == 2
