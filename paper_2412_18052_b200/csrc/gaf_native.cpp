@@ -341,6 +341,11 @@ PyObject *py_stream_end(PyObject *, PyObject *const *a, Py_ssize_t n) {
     PyErr_Format(PyExc_ValueError, "%s %s", what, text);
     throw Failed();
 }
+bool truth(PyObject *o) {
+    const int t = PyObject_IsTrue(o);
+    if (t < 0) throw Failed();          // (what an object's own conversion raised)
+    return t == 1;
+}
 // A tensor on the current device, whose stream the call will use.
 const at::Tensor &cuda_tensor(PyObject *o, const char *what) {
     const at::Tensor &t = tensor(o);
@@ -536,7 +541,7 @@ PyObject *py_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const Matrix residual(a[2], "residual");
         same_shape(residual, x.rows, x.cols, x.dtype, "residual");
         const double eps = number(a[3]);
-        const bool want_y = PyObject_IsTrue(a[4]) == 1, coded_y = PyObject_IsTrue(a[9]) == 1;
+        const bool want_y = truth(a[4]), coded_y = truth(a[9]);
         const std::vector<int64_t> shape = shape_with(*x.t, false, -1), rows = shape_with(*x.t, true, -1);
         const at::ScalarType type = x.t->scalar_type();
         const at::Device device = x.t->device();

@@ -112,3 +112,21 @@ def test_workload_with_a_wait_that_ran_out_is_refused():
     finally:
         gaf.gaf_test_set_wait_fault(0, False)
     assert len(workloads.language_model(2, 300, 128, 100).grads) == 2
+
+
+# --------------------------------------------------------------- arguments ----
+
+class NoTruth:
+    def __bool__(self):
+        raise ArithmeticError("neither")
+
+
+def test_flags_that_have_no_truth_value():
+    """What a flag's own conversion raises reaches the caller, and nothing is written."""
+    x, w = randn(gen(1), 5, 64), torch.ones(64, device="cuda")
+    for name in ("want_y", "coded_y"):
+        y, ck = torch.full((5, 64), 7.0, device="cuda"), gaf.new_checkpoint(5, 64)
+        ck[0].zero_()
+        with pytest.raises(ArithmeticError):
+            gaf.gaf_rms_norm(x, w, y=y, y_checkpoint=ck, **{name: NoTruth()})
+        assert bool((y == 7.0).all()) and not bool(ck[0].any())
