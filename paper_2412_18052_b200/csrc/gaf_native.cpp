@@ -16,6 +16,7 @@
 
 #include <cstdint>
 #include <new>
+#include <optional>
 #include <vector>
 
 #include "../../include/gaf.h"
@@ -430,18 +431,22 @@ struct LayerOutput {
         return o;
     }
 };
-// Codes and scales of a matrix of `rows` x `cols`: a pair of uint8 tensors, or None.
+// Codes and scales of a matrix of `rows` x `cols`: a pair of uint8 tensors, or None.  It holds the tensors until the call has been made: a
+// sequence may make them as they are asked for, and another thread may put others into a list.
 struct Checkpoint {
+    std::optional<Sequence> seq;
+    at::Tensor held[2];
     Matrix codes;
     uint8_t *scales = nullptr;
     Checkpoint(PyObject *o, const char *what, int64_t rows = -1, int64_t cols = -1) {
         if (o == Py_None) return;
-        const Sequence seq(o, true);
-        if (seq.n != 2) fail_value(what, "is a pair of codes and scales");
-        codes = Matrix(seq[0], what, at::kByte);
+        seq.emplace(o, true);
+        if (seq->n != 2) fail_value(what, "is a pair of codes and scales");
+        for (int i = 0; i < 2; ++i) held[i] = tensor((*seq)[i]);
+        codes = Matrix((*seq)[0], what, at::kByte);
         if (rows < 0) { rows = codes.rows; cols = codes.cols; }
         if (!codes.has(rows, cols)) fail_value(what, "has another shape than the call's matrices");
-        const at::Tensor &s = dense(seq[1], what, rows * ((cols + 127) / 128));
+        const at::Tensor &s = dense((*seq)[1], what, rows * ((cols + 127) / 128));
         if (s.scalar_type() != at::kByte) fail_value(what, "has scales that are not uint8");
         scales = static_cast<uint8_t *>(s.data_ptr());
     }

@@ -1,4 +1,6 @@
 """What the layers' calls leave for later calls to find, and what they do at the edges of their arguments."""
+import weakref
+
 import pytest
 import torch
 
@@ -130,3 +132,38 @@ def test_flags_that_have_no_truth_value():
         with pytest.raises(ArithmeticError):
             gaf.gaf_rms_norm(x, w, y=y, y_checkpoint=ck, **{name: NoTruth()})
         assert bool((y == 7.0).all()) and not bool(ck[0].any())
+
+
+class MadeWhenAsked:
+    """A pair whose items are made as they are asked for, and which notes how many launches the latest call had made when each was let go."""
+    def __init__(self, *pair):
+        self.pair, self.made, self.gone = pair, 0, {}
+
+    def __len__(self):
+        return 2
+
+    def __getitem__(self, i):
+        t = self.pair[i].view(self.pair[i].shape)               # (an object of its own)
+        weakref.finalize(t, lambda k: self.gone.__setitem__(k, gaf.gaf_last_launch_count()), self.made)
+        self.made += 1
+        return t
+
+
+def test_a_checkpoint_is_held_until_the_launch():
+    L = Layers()
+    ws, out = gaf.new_layer_workspace(L.T, L.d, gaf.GAF_F32), torch.empty(L.d, L.d, device="cuda")
+    other, third = gaf.new_checkpoint(L.T, L.d), gaf.new_checkpoint(L.T, L.d)
+
+    def norm(pair):
+        gaf.gaf_rms_norm(L.h, L.w, y_checkpoint=pair, h_checkpoint=third)
+        assert torch.equal(third[0], L.ck[0]) and torch.equal(third[1], L.ck[1])
+    for call, launches, pair in ((lambda p: gaf.gaf_linear_weight_grad(L.dy, p, out, ws), 3, L.ck),
+                                 (lambda p: gaf.gaf_checkpoint_unpack(p, out=torch.empty(L.T, L.d, device="cuda")), 1, L.ck),
+                                 (lambda p: gaf.gaf_checkpoint_pack(L.h, p), 1, other), (norm, 1, other)):
+        made = MadeWhenAsked(*pair)
+        gaf.gaf_embedding_grad(L.dy, L.tokens, torch.empty(L.V, L.d, device="cuda"), gaf.new_layer_workspace(L.T, L.d, gaf.GAF_F32, V=L.V))
+        assert gaf.gaf_last_launch_count() == 2
+        call(made)
+        assert gaf.gaf_last_launch_count() == launches
+        # (the first item is asked for once more to begin with, to see whether the pair can be indexed)
+        assert made.made >= 3 and all(made.gone[k] == launches for k in range(1, 3)), made.gone
