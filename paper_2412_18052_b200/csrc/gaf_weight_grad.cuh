@@ -150,9 +150,18 @@ __device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile
     *abort_flag = 1;
     return false;
 }
+// A warp's wait for one barrier, which every lane polls.
 template <int nap>
 __device__ __forceinline__ bool wg_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
     return __all_sync(0xFFFFFFFFu, wg_wait<nap>(bar, parity, abort_flag, limit)) != 0;
+}
+// A warp's wait for barriers that its lanes poll side by side.  The vote orders no memory: what one lane's barrier guards, the others may read behind
+// the warp barrier only (492 -> 500 us at the size above).
+template <int nap>
+__device__ __forceinline__ bool wg_wait_lanes(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
+    const bool ok = __all_sync(0xFFFFFFFFu, wg_wait<nap>(bar, parity, abort_flag, limit)) != 0;
+    __syncwarp();
+    return ok;
 }
 // One lane's arrival for its whole warp, here or at the same place in the pair's first CTA.
 __device__ __forceinline__ void wg_arrive_warp(uint64_t *bar) {
@@ -352,7 +361,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             const int shift = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
             for (int step = w.step0; step < w.step1; ++step) {
                 // (two lanes poll the codes' barrier and that of the place they go to)
-                if (!wg_wait_warp<kWgNapWiden>(lane == 0 ? &sh.code_full[s] : &sh.done[o], lane == 0 ? full_phase : wide_phase, &sh.abort_flag,
+                if (!wg_wait_lanes<kWgNapWiden>(lane == 0 ? &sh.code_full[s] : &sh.done[o], lane == 0 ? full_phase : wide_phase, &sh.abort_flag,
                                                a.spin_limit)) { alive = false; break; }
                 const unsigned char *const codes = code_ring + s * kWgCodeBytes;
                 unsigned char *const wide = wide_ring + o * kWgWideBytes;
@@ -434,7 +443,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     for (int step = w.step0; step < w.step1; ++step) {
                         const uint32_t buf = chain & 1u;
                         if (in_chain == 0 && !wg_wait_warp<kWgNapMma>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        if (!wg_wait_warp<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
+                        if (!wg_wait_lanes<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
                             alive = false;
                             break;
                         }
@@ -472,7 +481,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 for (int item = pair; item < a.items && alive; item += pairs) {
                     const WgItem w = wg_item(a, item, rank);
                     for (int step = w.step0; step < w.step1; ++step) {
-                        if (!wg_wait_warp<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : &sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!wg_wait_lanes<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : &sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                         tc_fence_async_smem();
                         wg_arrive_warp_in_first(&sh.other[o]);
                         if (++o == kWgRing) { o = 0; phase ^= 1u; }
