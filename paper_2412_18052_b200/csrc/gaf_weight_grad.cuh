@@ -74,6 +74,7 @@ struct WgShared {
     uint64_t code_full[kWgCodeRing], code_empty[kWgCodeRing];
     uint64_t dy_full[kWgRing], wide_full[kWgRing], done[kWgRing];  // done: the MMAs have read dy and the widened codes
     uint64_t other[kWgRing];                            // the second CTA's steps that are ready for the MMAs, in the first one
+    uint32_t told[kWgRing];                             // where the second CTA's words go
     uint64_t acc_full[2], acc_empty[2];                 // chains (acc_empty: of both CTAs, in the first one)
     uint64_t drained;
     uint32_t scale[kWgCodeRing][kWgK];                  // the word that holds each token's scale byte
@@ -132,17 +133,27 @@ __device__ __forceinline__ bool wg_elected() {
 // Bounded waits.  An attempt returns within tens of clocks whether or not the phase is complete, and a warp that polls takes issue
 // slots from the widening warps: who can afford it sleeps between attempts (`nap` nanoseconds).  A warp polls, and arrives, without
 // branching on the lane: after `if (lane == 0) ..` it went on in two parts, and executed everything twice (1223 -> 868 us at 16384 x 4096 x 4096).
-template <int nap>
+// kCluster: for barriers that the other CTA's threads count on.
+template <int nap, bool kCluster = false>
 __device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
     for (unsigned int spin = 0; spin < limit; ++spin) {
         uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(tc_smem_u32(bar)), "r"(parity)
-            : "memory");
+        if (kCluster)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(tc_smem_u32(bar)), "r"(parity)
+                : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(tc_smem_u32(bar)), "r"(parity)
+                : "memory");
         if (ok) return true;
         if (nap > 0) __nanosleep(nap);
         if ((spin & 15u) == 15u && *abort_flag) return false;
@@ -151,30 +162,40 @@ __device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile
     return false;
 }
 // A warp's wait for one barrier, which every lane polls.
-template <int nap>
+template <int nap, bool kCluster = false>
 __device__ __forceinline__ bool wg_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
-    return __all_sync(0xFFFFFFFFu, wg_wait<nap>(bar, parity, abort_flag, limit)) != 0;
+    return __all_sync(0xFFFFFFFFu, wg_wait<nap, kCluster>(bar, parity, abort_flag, limit)) != 0;
 }
 // A warp's wait for barriers that its lanes poll side by side.  The vote orders no memory: what one lane's barrier guards, the others may read behind
 // the warp barrier only (492 -> 500 us at the size above).
-template <int nap>
+template <int nap, bool kCluster = false>
 __device__ __forceinline__ bool wg_wait_lanes(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
-    const bool ok = __all_sync(0xFFFFFFFFu, wg_wait<nap>(bar, parity, abort_flag, limit)) != 0;
+    const bool ok = __all_sync(0xFFFFFFFFu, wg_wait<nap, kCluster>(bar, parity, abort_flag, limit)) != 0;
     __syncwarp();
     return ok;
 }
-// One lane's arrival for its whole warp, here or at the same place in the pair's first CTA.
+// One lane's arrival for its whole warp.
 __device__ __forceinline__ void wg_arrive_warp(uint64_t *bar) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "elect.sync _|p, 0xFFFFFFFF;\n\t"
         "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(tc_smem_u32(bar)) : "memory");
 }
+// An arrival at this place in the pair's first CTA that hands on what the fences of tcgen05 order: that this warp has read tensor memory.
 __device__ __forceinline__ void wg_arrive_warp_in_first(uint64_t *bar) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "elect.sync _|p, 0xFFFFFFFF;\n\t"
-        "@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}" ::"r"(wg_in_first(bar)) : "memory");
+        "@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(wg_in_first(bar)) : "memory");
+}
+// One lane tells the first CTA what this CTA has in shared memory: a word stored there asynchronously, whose 4 bytes complete the barrier's phase with
+// release semantics at cluster scope.  (An arrival with release semantics takes hundreds of clocks a step: 581 us against 488 at the size above.)
+__device__ __forceinline__ void wg_tell_first(uint32_t *word, uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "@p st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];\n\t}" ::"r"(wg_in_first(word)), "r"(1u), "r"(wg_in_first(bar))
+        : "memory");
 }
 // 32 lanes x 8 columns of accumulators.
 __device__ __forceinline__ void wg_tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
@@ -274,7 +295,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             tc_mbar_init(&sh.dy_full[s], 1);
             tc_mbar_init(&sh.wide_full[s], 8);
             tc_mbar_init(&sh.done[s], 1);
-            tc_mbar_init(&sh.other[s], 1);
+            tc_mbar_init(&sh.other[s], 1);               // (armed for the next word)
         }
         for (int b = 0; b < 2; ++b) {
             tc_mbar_init(&sh.acc_full[b], 1);
@@ -283,6 +304,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         tc_mbar_init(&sh.drained, 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < kWgRing; ++s) tc_mbar_arrive_expect_tx(&sh.other[s], sizeof(uint32_t));
     }
     if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc_smem_u32(&sh.tmem_base)), "r"(kWgTmemCols)
@@ -442,8 +464,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     int in_chain = 0;
                     for (int step = w.step0; step < w.step1; ++step) {
                         const uint32_t buf = chain & 1u;
-                        if (in_chain == 0 && !wg_wait_warp<kWgNapMma>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        if (!wg_wait_lanes<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
+                        if (in_chain == 0 && !wg_wait_warp<kWgNapMma, true>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!wg_wait_lanes<kWgNapMma, true>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
                             alive = false;
                             break;
                         }
@@ -451,6 +473,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                         tc_fence_after_sync();
                         const bool last = in_chain == kWgChunkSteps - 1 || step + 1 == w.step1;
                         if (wg_elected()) {
+                            tc_mbar_arrive_expect_tx(&sh.other[o], sizeof(uint32_t));
                             const uint64_t a0 = da + (uint64_t)(o * (kWgWideBytes / 16)), b0 = db + (uint64_t)(o * (kWgDyBytes / 16));
 #pragma unroll
                             for (int k = 0; k < kWgK / 16; ++k)       // 16 tokens = 2048 bytes on
@@ -483,7 +506,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     for (int step = w.step0; step < w.step1; ++step) {
                         if (!wg_wait_lanes<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : &sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                         tc_fence_async_smem();
-                        wg_arrive_warp_in_first(&sh.other[o]);
+                        wg_tell_first(&sh.told[o], &sh.other[o]);
                         if (++o == kWgRing) { o = 0; phase ^= 1u; }
                     }
                 }

@@ -30,3 +30,17 @@ def test_a_vote_over_different_barriers_is_followed_by_a_warp_barrier():
     assert not [c for c in calls(text, r"(?:wg_wait_warp|wg_wait)") if "lane" in c]
     body = text[text.index("bool wg_wait_lanes"):]
     assert re.match(r"[^}]*__all_sync\([^;]*;\s*__syncwarp\(\);\s*return", body)
+
+
+def test_what_passes_between_the_ctas_of_a_pair_is_ordered_at_cluster_scope():
+    """Arrivals and waits without a scope order nothing beyond their CTA.  What the second CTA has in shared memory is told by a store whose completion
+    releases at cluster scope; that tensor memory was read is ordered by the fences of tcgen05, at cluster scope too; the first CTA's waits acquire there."""
+    text = source("gaf_weight_grad.cuh")
+    assert "mbarrier.arrive.shared::cluster" not in text
+    remote = re.findall(r"mbarrier\.arrive\S*shared::cluster\S*", text)
+    assert remote and all(".cluster.shared::cluster" in r for r in remote)
+    assert all("sh.other" in c for c in calls(text, r"(?<!void )wg_tell_first")) and "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes" in text
+    assert all("sh.acc_empty" in c for c in calls(text, r"(?<!void )wg_arrive_warp_in_first"))
+    waits = re.findall(r"wg_wait\w*<[^<>]*>\([^;]*", text)
+    crossing = [w for w in waits if "sh.other" in w or "sh.acc_empty" in w]
+    assert len(crossing) == 2 and all(re.match(r"wg_wait\w*<\w+, true>", w) for w in crossing)
