@@ -10,7 +10,8 @@
 //   group + fill   One cluster puts the positions of equal tokens next to one another (counts, places, positions; its steps are
 //            separated by cluster barriers).  Integer atomics hand out the places, so which position stands where inside a token's
 //            stretch differs from run to run; stretches of more than 32 are therefore put in ascending order here (a warp each, a
-//            bit per position), shorter ones by the warp that adds them.  All other CTAs meanwhile write the rows of tokens that do
+//            bit per position; in texts of more than 32,768 tokens window by window, its positions put together first: two tokens in 2 M
+//            positions 8.2 ms, 73 ms where every window looked through all of them), shorter ones by the warp that adds them.  All other CTAs meanwhile write the rows of tokens that do
 //            not occur, of the first half of the table, each after looking through the tokens for those of its own range.  (Grouping first, then one
 //            kernel that met every row and looked up its count: 67.6 and 479 us where this takes 36 and 328, at 1000
 //            tokens, 50,257 x 768 binary32, and 32,768 tokens, 100,000 x 2048 with a base.)
@@ -70,9 +71,13 @@ constexpr int kGroupCtas = 8;                   // of a cluster
 constexpr int kGroupThreads = 1024;
 constexpr int kLightMost = 32;                  // longest stretch that one warp orders and adds
 constexpr int kOrderWords = 1024;               // positions whose bits a warp holds at once, / 32
+constexpr int kOrderWindow = kOrderWords * 32;
+constexpr int kOrderWindows = 512;              // windows whose counts a warp holds at once, where the text is longer than one
 constexpr int kFillRows = 1 << 16;              // rows whose bits a filling CTA holds at once
-constexpr int kGroupSmem = kGroupThreads / 32 * kOrderWords * 4;
-static_assert(kFillRows / 8 <= kGroupSmem, "the bits of the rows fit where the bits of the positions do");
+__host__ __device__ constexpr int order_words(bool one_window) { return one_window ? kOrderWords : kOrderWords + kOrderWindows; }
+// (a text within one window leaves the rest to the L1 cache)
+__host__ __device__ constexpr int group_smem_bytes(bool one_window) { return kGroupThreads / 32 * order_words(one_window) * 4; }
+static_assert(kFillRows / 8 <= group_smem_bytes(true), "the bits of the rows fit where the bits of the positions do");
 
 // A token with a short stretch; a piece of a long one (everything that its sum needs, in one or two loads): its token, first place and
 // positions, which long stretch it belongs to, and that one's pieces.
@@ -114,6 +119,39 @@ __device__ __forceinline__ unsigned int warp_scan(unsigned int v, int lane) {   
         if (lane >= o) v += below;
     }
     return v;
+}
+
+// f of each of n positions, and of 0xFFFFFFFF, in any order.  (Sixteen loads in flight: one after the other, a text's most frequent token took
+// longer than all else here.)
+template <typename F>
+__device__ __forceinline__ void each_position(const unsigned int *from, unsigned int n, int lane, F &&f) {
+    for (unsigned int k0 = lane; k0 < n; k0 += 32 * 16) {
+        unsigned int at[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) at[j] = k0 + 32 * j < n ? __ldcg(from + k0 + 32 * j) : 0xFFFFFFFFu;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f(at[j]);
+    }
+}
+// n positions, all of the window of 32 * words that starts at p0, in ascending order: a bit per position, read back in order.  `to` may be `from`.
+__device__ __forceinline__ void order_window(unsigned int *bits, const unsigned int *from, unsigned int n, unsigned int p0, int words, unsigned int *to,
+                                             int lane) {
+    for (int w = lane; w < words; w += 32) bits[w] = 0u;
+    __syncwarp();
+    each_position(from, n, lane, [&](unsigned int p) {
+        if (p != 0xFFFFFFFFu) atomicOr(bits + ((p - p0) >> 5), 1u << (p & 31u));
+    });
+    __syncwarp();
+    unsigned int done = 0u;
+    for (int w0 = 0; w0 < words; w0 += 32) {
+        const unsigned int word = w0 + lane < words ? bits[w0 + lane] : 0u;
+        const unsigned int sum = warp_scan((unsigned int)__popc(word), lane);
+        unsigned int at = done + sum - (unsigned int)__popc(word);
+        const unsigned int base = p0 + (unsigned int)(w0 + lane) * 32u;
+        for (unsigned int b = word; b != 0u; b &= b - 1u) to[at++] = base + (unsigned int)(__ffs(b) - 1);
+        done += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    __syncwarp();
 }
 
 template <typename I>
@@ -199,38 +237,54 @@ __device__ __forceinline__ void group_tokens(const EmbedGradArgs &a, unsigned in
         if (v >= 0) a.pos[__ldcg(a.start + v) + a.slot[t]] = (unsigned int)t;
     }
     cluster_barrier();
-    // ascending order of the long stretches: a bit per position, read back in order
-    unsigned int *const bits = smem + (threadIdx.x >> 5) * kOrderWords;
+    // ascending order of the long stretches
+    const bool one_window = a.T <= kOrderWindow;
+    unsigned int *const bits = smem + (threadIdx.x >> 5) * order_words(one_window), *const count = bits + kOrderWords;
     const unsigned int heavies = __ldcg(&a.cur->heavies);
     for (unsigned int h = (unsigned int)(tid >> 5); h < heavies; h += (unsigned int)(kThreads >> 5)) {
         const unsigned int v = __ldcg(a.heavy + h);
         const unsigned int n = __ldcg(a.count + v), first = __ldcg(a.start + v);
-        unsigned int done = first;
-        for (int64_t t0 = 0; t0 < a.T; t0 += (int64_t)kOrderWords * 32) {
-            const int words = (int)min((int64_t)kOrderWords, (a.T - t0 + 31) / 32);
-            for (int w = lane; w < words; w += 32) bits[w] = 0u;
+        const unsigned int *const from = a.pos + first;
+        unsigned int *to = a.ordered + first;
+        if (one_window) {
+            order_window(bits, from, n, 0u, (int)((a.T + 31) / 32), to, lane);
+            continue;
+        }
+        // 512 windows at a time: the positions of each are put together, in any order, and then set right within the window
+        for (int64_t t0 = 0; t0 < a.T; t0 += (int64_t)kOrderWindow * kOrderWindows) {
+            auto window = [&](unsigned int p) {              // of a position, or none of these
+                const int64_t w = ((int64_t)p - t0) / kOrderWindow;
+                return p != 0xFFFFFFFFu && (int64_t)p >= t0 && w < kOrderWindows ? (int)w : -1;
+            };
+            for (int w = lane; w < kOrderWindows; w += 32) count[w] = 0u;
             __syncwarp();
-            // (sixteen loads in flight: one after the other, a text's most frequent token took longer than all else here)
-            for (unsigned int k0 = lane; k0 < n; k0 += 32 * 16) {
-                unsigned int at[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) at[j] = k0 + 32 * j < n ? __ldcg(a.pos + first + k0 + 32 * j) : 0xFFFFFFFFu;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int64_t p = (int64_t)at[j] - t0;
-                    if (p >= 0 && p < (int64_t)kOrderWords * 32 && at[j] != 0xFFFFFFFFu) atomicOr(bits + (p >> 5), 1u << (p & 31));
+            each_position(from, n, lane, [&](unsigned int p) {
+                const int w = window(p);
+                if (w >= 0) atomicAdd(count + w, 1u);
+            });
+            __syncwarp();
+            unsigned int before = 0u;                        // counts become places
+            for (int w0 = 0; w0 < kOrderWindows; w0 += 32) {
+                const unsigned int c = count[w0 + lane], sum = warp_scan(c, lane);
+                count[w0 + lane] = before + sum - c;
+                before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+            }
+            __syncwarp();
+            each_position(from, n, lane, [&](unsigned int p) {
+                const int w = window(p);
+                if (w >= 0) to[atomicAdd(count + w, 1u)] = p;
+            });
+            __syncwarp();                                    // (and every place is now the next window's first)
+            for (int w0 = 0; w0 < kOrderWindows; w0 += 32) {
+                const unsigned int end = count[w0 + lane], begin = w0 + lane == 0 ? 0u : count[w0 + lane - 1];
+                for (unsigned int some = __ballot_sync(0xFFFFFFFFu, end != begin); some != 0u; some &= some - 1u) {
+                    const int k = __ffs(some) - 1;
+                    const unsigned int b = __shfl_sync(0xFFFFFFFFu, begin, k), e = __shfl_sync(0xFFFFFFFFu, end, k);
+                    const unsigned int p0 = (unsigned int)(t0 + (int64_t)(w0 + k) * kOrderWindow);
+                    order_window(bits, to + b, e - b, p0, (int)min((int64_t)kOrderWords, (a.T - p0 + 31) / 32), to + b, lane);
                 }
             }
-            __syncwarp();
-            for (int w0 = 0; w0 < words; w0 += 32) {
-                const unsigned int word = w0 + lane < words ? bits[w0 + lane] : 0u;
-                const unsigned int sum = warp_scan((unsigned int)__popc(word), lane);
-                unsigned int at = done + sum - (unsigned int)__popc(word);
-                const unsigned int base = (unsigned int)(t0 + (int64_t)(w0 + lane) * 32);
-                for (unsigned int b = word; b != 0u; b &= b - 1u) a.ordered[at++] = base + (unsigned int)(__ffs(b) - 1);
-                done += __shfl_sync(0xFFFFFFFFu, sum, 31);
-            }
-            __syncwarp();
+            to += before;
         }
     }
 }

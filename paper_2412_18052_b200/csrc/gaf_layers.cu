@@ -183,9 +183,9 @@ int launch_embedding_grad(const EmbedGradArgs &a, int dtype, int grad_dtype, int
         struct Plan { int group = 0, f32 = 0, bf16 = 0; };
         static PerDevice<Plan> table;
         GAF_TRY(plan_once(table.plan[di.dev], table.ready[di.dev], [&](Plan &pl) {
-            if (cudaFuncSetAttribute(group, cudaFuncAttributeMaxDynamicSharedMemorySize, kGroupSmem) != cudaSuccess) return int(GAF_ERR_CUDA);
+            if (cudaFuncSetAttribute(group, cudaFuncAttributeMaxDynamicSharedMemorySize, group_smem_bytes(false)) != cudaSuccess) return int(GAF_ERR_CUDA);
             cudaLaunchConfig_t cfg{};
-            cfg.gridDim = dim3(kGroupCtas); cfg.blockDim = dim3(kGroupThreads); cfg.dynamicSmemBytes = kGroupSmem;
+            cfg.gridDim = dim3(kGroupCtas); cfg.blockDim = dim3(kGroupThreads); cfg.dynamicSmemBytes = group_smem_bytes(false);
             int clusters = 0, f32 = 0, bf16 = 0;
             if (cudaOccupancyMaxActiveClusters(&clusters, group, &cfg) != cudaSuccess || clusters < 1 ||
                 cudaOccupancyMaxActiveBlocksPerMultiprocessor(&f32, sum_f32, kEmbedWarps * 32, 0) != cudaSuccess || f32 < 1 ||
@@ -195,7 +195,8 @@ int launch_embedding_grad(const EmbedGradArgs &a, int dtype, int grad_dtype, int
             return int(GAF_OK);
         }));
         const Plan &pl = table.plan[di.dev];
-        cudaError_t err = launch_dependent_smem(group, a.base == a.grad ? kGroupCtas : pl.group, kGroupThreads, size_t(kGroupSmem), st, a);
+        cudaError_t err = launch_dependent_smem(group, a.base == a.grad ? kGroupCtas : pl.group, kGroupThreads,
+                                                size_t(group_smem_bytes(a.T <= kOrderWindow)), st, a);
         if (err != cudaSuccess) return launched(err, 1);
         const int64_t need = ceil_div(3 * std::max(a.T * a.tiles, a.V / 8), kEmbedWarps);
         auto grid = [&](int resident) { return int(std::min<int64_t>(resident, need) / 3 * 3 + 3); };

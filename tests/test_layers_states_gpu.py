@@ -1,4 +1,5 @@
 """What the layers' calls leave for later calls to find, and what they do at the edges of their arguments."""
+import math
 import weakref
 
 import pytest
@@ -167,3 +168,47 @@ def test_a_checkpoint_is_held_until_the_launch():
         assert gaf.gaf_last_launch_count() == launches
         # (the first item is asked for once more to begin with, to see whether the pair can be indexed)
         assert made.made >= 3 and all(made.gone[k] == launches for k in range(1, 3)), made.gone
+
+
+# -------------------------------------------------------------- long texts ----
+
+def time_of(call, n=3):
+    call()
+    best = math.inf
+    for _ in range(n):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        call()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+def test_embedding_grad_of_two_tokens_grows_with_the_text():
+    """Two tokens that make up a text of a million and more positions (segment numbers, say): four times the text takes about four times as long, not sixteen."""
+    V, d, ms = 2, 8, {}
+    for T in (1 << 19, 1 << 21):
+        dy = randn(gen(3), T, d, dtype=torch.bfloat16)
+        tokens = torch.randint(0, V, (T,), generator=gen(4), device="cuda")
+        ws, grad = gaf.new_layer_workspace(T, d, gaf.GAF_BF16, V=V), torch.empty(V, d, device="cuda")
+        ms[T] = time_of(lambda: gaf.gaf_embedding_grad(dy, tokens, grad, ws))
+    print("ms", ms)
+    assert ms[1 << 21] < 8 * ms[1 << 19], ms
+
+
+@pytest.mark.parametrize("T,V,d", [(32_768, 3, 8), (32_769, 3, 8), (65_536, 2, 5), (98_310, 700, 24), (200_000, 5000, 8), (16_777_217, 3, 1), (17_000_000, 2, 1)])
+def test_embedding_grad_of_long_texts(T, V, d):
+    """Texts of one window of the ordering (32,768 positions), of several, and of more than 512: whole numbers, whose sums are exact; and the same bits again
+    and again for others, whatever order the counters handed out."""
+    g = gen(T + V)
+    tokens = torch.randint(-1, V, (T,), generator=g, device="cuda")
+    ws = gaf.new_layer_workspace(T, d, gaf.GAF_BF16, V=V)
+    whole = torch.randint(-1, 2, (T, d), generator=g, device="cuda").to(torch.bfloat16)
+    want = torch.zeros(V + 1, d, dtype=torch.float64, device="cuda").index_add_(0, torch.where(tokens < 0, V, tokens), whole.double())[:V]
+    assert bool((want.abs() < 2 ** 24).all())
+    assert torch.equal(gaf.gaf_embedding_grad(whole, tokens, torch.empty(V, d, device="cuda"), ws).double(), want)
+    dy = randn(g, T, d, dtype=torch.bfloat16)
+    first = gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws)
+    for _ in range(3):
+        assert torch.equal(first, gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws))
