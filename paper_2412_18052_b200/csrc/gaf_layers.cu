@@ -288,10 +288,12 @@ extern "C" {
 int gaf_layer_workspace_bytes(int64_t T, int64_t width, int64_t V, int dtype, size_t *bytes_out) {
     if (!bytes_out || !in_range(T) || !in_range(width) || !in_range(V) || !is_dtype(dtype)) return GAF_ERR_ARG;
     // a weight gradient of at most width x width: the partial sums of split tokens are never more than this many tiles
-    const int64_t tiles = std::min(kWgMaxSplitItems, ceil_div(width, kWgPairM) * ceil_div(width, kWgN) *
-                                                               ceil_div(T, kWgK) * (dtype == GAF_F32 ? 3 : 1));
+    const int64_t terms = dtype == GAF_F32 ? 3 : 1, side = std::min(kWgMaxSplitItems, ceil_div(width, kWgN)),
+                  tiles = std::min(kWgMaxSplitItems, side * side * std::min(kWgMaxSplitItems, ceil_div(T, kWgK) * terms));
     size_t wg = kLayerScratchOffset + size_t(tiles) * kWgPairM * kWgN * 4 + 256;
-    wg += size_t(dtype == GAF_F32 ? 3 : 1) * round_up(size_t(T), kWgK) * round_up(size_t(width), 8) * 2;
+    const size_t rows = size_t(terms) * round_up(size_t(T), kWgK), pitch = round_up(size_t(width), 8) * 2;
+    if (pitch > 0 && rows > (SIZE_MAX / 2) / pitch) return GAF_ERR_TOO_LARGE;
+    wg += rows * pitch;
     const size_t a = embed_layout(T, width, V).end, b = norm_grad_bytes(width);
     *bytes_out = round_up(std::max(wg, std::max(a, b)), 256);
     return GAF_OK;
