@@ -54,12 +54,13 @@ def _compile(force: bool, verbose: bool) -> None:
         if not force and _object_up_to_date(source):
             continue
         obj, tmp = _object_of(source), _object_of(source) + f".{os.getpid()}.tmp.o"
-        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-MD", "-MF", obj + ".d", "-c", source, "-o", tmp]
+        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-MD", "-MF", tmp + ".d", "-c", source, "-o", tmp]
         running.append((subprocess.Popen(cmd), cmd, tmp, obj))
     codes = [p.wait() for p, _, _, _ in running]
     for rc, (_, cmd, tmp, obj) in zip(codes, running):
         if rc != 0:
             raise subprocess.CalledProcessError(rc, cmd)
+        os.replace(tmp + ".d", obj + ".d")      # (whole, and before the object: never an object with an older list)
         os.replace(tmp, obj)
 
 
