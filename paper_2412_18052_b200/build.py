@@ -34,13 +34,15 @@ def _object_of(source: str) -> str:
 
 
 def _object_up_to_date(source: str) -> bool:
-    """Whether a source's object is newer than everything that went into it (the list that nvcc left beside it)."""
+    """Whether a source's object is newer than everything that went into it (the list that nvcc left beside it, which names
+    another tree's files where the object was copied along)."""
     obj = _object_of(source)
     try:
         with open(obj + ".d") as f:
             parts = f.read().replace("\\\n", " ").split()
         made = os.path.getmtime(obj)
-        return all(os.path.getmtime(p) <= made for p in parts[1:] if p != ":")
+        parts = [p for p in parts[1:] if p != ":"]
+        return parts[:1] == [source] and all(os.path.getmtime(p) <= made for p in parts)
     except OSError:
         return False
 

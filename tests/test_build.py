@@ -58,3 +58,13 @@ def test_a_compilation_that_does_not_end_leaves_the_object_with_its_whole_list(t
         b._compile(True, False)
     os.utime(tree / "a.cuh")
     assert not b._object_up_to_date(b.SOURCES[0])
+
+
+def test_an_object_of_another_tree_is_not_taken(tree, monkeypatch):
+    """A copied tree brings objects along, with lists of the first one's files: changes in the copy would not show."""
+    b._compile(False, False)
+    copy = tree / "copy"
+    copy.mkdir()
+    (copy / "s.cu").write_text("// changed")
+    os.utime(copy / "s.cu", (1e9, 1e9))
+    assert not b._object_up_to_date(str(copy / "s.cu"))
