@@ -18,7 +18,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def _newest_source_mtime() -> float:
-    newest = 0.0
+    newest = os.path.getmtime(__file__)                 # (the flags stand here)
     for root in (CSRC, os.path.join(os.path.dirname(HERE), "include")):
         for name in os.listdir(root):
             newest = max(newest, os.path.getmtime(os.path.join(root, name)))
@@ -42,7 +42,7 @@ def _object_up_to_date(source: str) -> bool:
             parts = f.read().replace("\\\n", " ").split()
         made = os.path.getmtime(obj)
         parts = [p for p in parts[1:] if p != ":"]
-        return parts[:1] == [source] and all(os.path.getmtime(p) <= made for p in parts)
+        return os.path.getmtime(__file__) <= made and parts[:1] == [source] and all(os.path.getmtime(p) <= made for p in parts)
     except OSError:
         return False
 

@@ -68,3 +68,15 @@ def test_an_object_of_another_tree_is_not_taken(tree, monkeypatch):
     (copy / "s.cu").write_text("// changed")
     os.utime(copy / "s.cu", (1e9, 1e9))
     assert not b._object_up_to_date(str(copy / "s.cu"))
+
+
+def test_other_flags_make_everything_anew(tree):
+    """The flags stand in build.py: what is older than it is not current."""
+    b._compile(False, False)
+    then = os.path.getmtime(b.__file__) - 10
+    os.utime(b._object_of(b.SOURCES[0]), (then, then))
+    assert not b._object_up_to_date(b.SOURCES[0])
+    lib = tree / "lib.so"
+    lib.write_text("")
+    os.utime(lib, (then, then))
+    assert not b._up_to_date(str(lib))
