@@ -83,15 +83,20 @@ template <int N> struct Count { static constexpr int value = N; };
 // Threads per row and tiles per warp of the norm's kernels, by the width: as few threads as hold the row in registers.  The backward pass has
 // three times as much to hold and takes twice the threads (16384 x 4096 bfloat16: forward 95 us with 128 threads, 103 with 256;
 // backward from codes 105 and 95).
-template <typename F>
-int by_width(int64_t d, bool backward, F &&f) {
+template <bool BACKWARD, typename F>
+int by_width(int64_t d, F &&f) {
     if (d <= 256) return f(Count<32>(), Count<1>());
     if (d <= 512) return f(Count<32>(), Count<2>());
     if (d <= 768) return f(Count<32>(), Count<3>());
     if (d <= 1024) return f(Count<32>(), Count<4>());
     if (d <= 2048) return f(Count<128>(), Count<2>());
-    if (d <= 4096) return backward ? f(Count<256>(), Count<2>()) : f(Count<128>(), Count<4>());
-    if (d <= 8192) return backward ? f(Count<512>(), Count<2>()) : f(Count<256>(), Count<4>());
+    if constexpr (BACKWARD) {
+        if (d <= 4096) return f(Count<256>(), Count<2>());
+        if (d <= 8192) return f(Count<512>(), Count<2>());
+    } else {
+        if (d <= 4096) return f(Count<128>(), Count<4>());
+        if (d <= 8192) return f(Count<256>(), Count<4>());
+    }
     return f(Count<512>(), Count<4>());
 }
 
@@ -207,7 +212,7 @@ int launch_embedding_grad(const EmbedGradArgs &a, int dtype, int grad_dtype, int
 }
 
 int launch_rms_norm(const NormArgs &a, int dtype, bool vec, cudaStream_t st) {
-    return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_width(a.d, false, [&](auto r, auto s) {
+    return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_width<false>(a.d, [&](auto r, auto s) {
         constexpr int R = decltype(r)::value;
         const int64_t ctas = ceil_div(a.T, norm_threads(R) / R);
         return launched(launch_dependent(rms_norm_kernel<typename decltype(t)::type, decltype(v)::value, R, decltype(s)::value>, int(ctas),
@@ -217,7 +222,7 @@ int launch_rms_norm(const NormArgs &a, int dtype, bool vec, cudaStream_t st) {
 
 int launch_rms_norm_grad(const NormGradArgs &a, NormFinishArgs f, int dtype, int grad_dtype, bool vec, const DeviceInfo &di, cudaStream_t st) {
     return by_type(dtype, [&](auto t) { return by_flag(vec, [&](auto v) { return by_flag(a.h_codes != nullptr, [&](auto coded) {
-        return by_width(a.d, true, [&](auto r, auto s) {
+        return by_width<true>(a.d, [&](auto r, auto s) {
             constexpr int R = decltype(r)::value;
             auto kernel = rms_norm_grad_kernel<typename decltype(t)::type, decltype(v)::value, decltype(coded)::value, R, decltype(s)::value>;
             // as many CTAs as the device holds at once, so that each sums as many rows as possible

@@ -1,6 +1,12 @@
-"""Rules of the memory model that no run can show: read from the kernels' sources."""
+"""Rules that no run can show: read from the kernels' sources, and from the names of what was compiled."""
 import os
 import re
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2412_18052_b200.build import LIB, build
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2412_18052_b200", "csrc")
 
@@ -44,3 +50,16 @@ def test_what_passes_between_the_ctas_of_a_pair_is_ordered_at_cluster_scope():
     waits = re.findall(r"wg_wait\w*<[^<>]*>\([^;]*", text)
     crossing = [w for w in waits if "sh.other" in w or "sh.acc_empty" in w]
     assert len(crossing) == 2 and all(re.match(r"wg_wait\w*<\w+, true>", w) for w in crossing)
+
+
+def test_every_variant_of_the_norm_is_one_that_some_width_takes():
+    """The norm's kernels are compiled for the numbers of threads and tiles that by_width hands out, and for no others."""
+    nm = shutil.which("nm")
+    if nm is None:
+        pytest.skip("no nm")
+    build()
+    names = subprocess.run([nm, "-C", LIB], capture_output=True, text=True, check=True).stdout
+    short = {(32, 1), (32, 2), (32, 3), (32, 4), (128, 2), (512, 4)}
+    for kernel, want in (("rms_norm_kernel", short | {(128, 4), (256, 4)}), ("rms_norm_grad_kernel", short | {(256, 2), (512, 2)})):
+        found = {(int(r), int(s)) for r, s in re.findall(r"gaf::" + kernel + r"<[^>]*, (\d+), (\d+)>", names)}
+        assert found == want, (kernel, found ^ want)
