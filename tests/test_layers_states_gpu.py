@@ -1,4 +1,5 @@
-"""What the layers' calls leave for later calls to find, and what they do at the edges of their arguments."""
+"""What the layers' calls leave for later calls to find, and what they do at the edges of their arguments: status words, values that are not finite,
+arguments of odd kinds, long texts."""
 import math
 import weakref
 
@@ -7,6 +8,8 @@ import torch
 
 import paper_2412_18052_b200 as gaf
 from paper_2412_18052_b200 import workloads
+import layer_reference as ref
+from layer_reference import TYPES, assert_close
 
 pytestmark = pytest.mark.gpu
 
@@ -212,3 +215,77 @@ def test_embedding_grad_of_long_texts(T, V, d):
     first = gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws)
     for _ in range(3):
         assert torch.equal(first, gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws))
+
+
+# ---------------------------------------------------- values not finite ----
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [264, 1001])
+def test_embedding_grad_of_values_that_are_not_finite(dtype, d):
+    """They reach their own column of their own token's row, in short and in long stretches; padding's reach nothing."""
+    t, g, T, V = TYPES[dtype], gen(d), 500, 40
+    dy = randn(g, T, d, dtype=t)
+    tokens = torch.randint(2, V, (T,), generator=g, device="cuda")
+    tokens[100:300] = 1                             # a long stretch
+    tokens[[3, 400]] = torch.tensor([0, -1], device="cuda")
+    dy[3, 5], dy[250, 7], dy[400] = float("nan"), float("inf"), float("nan")
+    dy[251, 9], dy[252, 9] = float("inf"), -float("inf")
+    base = randn(g, V, d)
+    base[2, 11], base[V - 1, 0] = float("nan"), -float("inf")
+    ws = gaf.new_layer_workspace(T, d, gaf.GAF_F32 if dtype == "f32" else gaf.GAF_BF16, V=V)
+    for b in (None, base):
+        got = gaf.gaf_embedding_grad(dy, tokens, torch.empty(V, d, device="cuda"), ws, scale=0.5, base=b)
+        want, off = ref.embedding_grad(dy, tokens, V, 0.5, b)
+        assert bool(torch.isnan(want[0, 5])) and bool(torch.isnan(want[1, 9])) and want[1, 7].item() == math.inf
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        fine = torch.isfinite(want)
+        assert torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
+        assert_close(got[fine], want[fine], off[fine])
+
+
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [264, 1001, 4096])
+def test_rms_norm_grad_of_values_that_are_not_finite(d, dtype, coded):
+    """They reach their own row of dx, through its mean, and the columns of dweight that they stand in."""
+    t, g, T = TYPES[dtype], gen(d + 1), 40
+    dy, h, w, res = randn(g, T, d, dtype=t), randn(g, T, d, dtype=t), randn(g, d, dtype=t), randn(g, T, d, dtype=t)
+    rstd = (h.double().square().mean(dim=1) + 1e-6).rsqrt().float()
+    dy[3, 5], dy[9, 100], h[20, 7], res[30, 8] = float("nan"), float("inf"), float("nan"), float("inf")
+    ck = gaf.gaf_checkpoint_pack(h)
+    hv = ref.checkpoint_values(ck) if coded else h.double()
+    dw = torch.empty(d, device="cuda")
+    ws = gaf.new_layer_workspace(T, d, gaf.GAF_F32 if dtype == "f32" else gaf.GAF_BF16)
+    dx, _ = gaf.gaf_rms_norm_grad(dy, ck if coded else h, w, rstd, dw, ws, residual_grad=res)
+    want, want_w, off, off_w = ref.rms_norm_grad(dy, hv, w, rstd, res)
+    rows = torch.ones(T, dtype=torch.bool, device="cuda")
+    rows[[3, 9, 20, 30]] = False
+    columns = torch.ones(d, dtype=torch.bool, device="cuda")
+    columns[[5, 7, 100]] = False
+    assert_close(dx[rows], want[rows], off[rows])
+    assert_close(dw[columns], want_w[columns], off_w[columns])
+    assert not bool(torch.isfinite(dw[~columns]).any()) and not bool(torch.isfinite(dx[[3, 9, 20]]).any())
+    assert dx[30, 8].item() == math.inf and bool(torch.isfinite(dx[30, :8]).all()) and bool(torch.isfinite(dx[30, 9:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layers_between_filter_calls_of_every_kind(dtype):
+    """One workspace for the layers and for filters that keep tags, hints and tickets in it from call to call: what a workspace of its own gives, bit for bit."""
+    L, D, code = Layers(), 50_000, gaf.GAF_F32 if dtype == "f32" else gaf.GAF_BF16
+    g = gen(7)
+    common = randn(g, D)
+    grads = [(common + randn(g, D)).to(TYPES[dtype]) for _ in range(40)]
+    shared = torch.empty(max(L.bytes(), gaf.gaf_workspace_bytes(40, D, code)), dtype=torch.uint8, device="cuda")
+    gaf.gaf_workspace_init(shared)
+    alone = gaf.new_workspace(40, D, code)
+    calls = [lambda ws, K=K: gaf.gaf_filter_accumulate(grads[:K], 0.6, ws) for K in (2, 3, 8, 9, 17, 40)]
+    calls += [lambda ws, K=K, s=s: gaf.gaf_filter_accumulate(grads[:K], 0.6, ws, schedule=s) for K in (2, 4) for s in (gaf.binding.GAF_SCHED_STEPWISE, gaf.binding.GAF_SCHED_GRAM)]
+    calls += [lambda ws, K=K: gaf.gaf_pairwise_cosdist(grads[:K], ws) for K in (2, 8, 17)]
+    calls += [lambda ws: gaf.gaf_filter_accumulate_bucketed(grads[:4], 0.6, [0, 16_000, 40_000, D], ws), lambda ws: gaf.gaf_filter_accumulate_any_seed(grads[:3], 0.6, ws)]
+    for turn in range(2):
+        for k, call in enumerate(calls):
+            for layer in L.calls():
+                layer(shared)
+            got, want = call(shared), call(alone)
+            assert all(torch.equal(a, b) for a, b in zip(got, want) if torch.is_tensor(a)), (turn, k)
+            assert gaf.gaf_read_status(shared) == gaf.gaf_read_status(alone), (turn, k)
