@@ -134,45 +134,46 @@ __device__ __forceinline__ bool wg_elected() {
 // slots from the widening warps: who can afford it sleeps between attempts (`nap` nanoseconds).  A warp polls, and arrives, without
 // branching on the lane: after `if (lane == 0) ..` it went on in two parts, and executed everything twice (1223 -> 868 us at 16384 x 4096 x 4096).
 // kCluster: for barriers that the other CTA's threads count on.
-template <int nap, bool kCluster = false>
-__device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
+template <bool kCluster = false>
+__device__ __forceinline__ uint32_t wg_try(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    if (kCluster)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(tc_smem_u32(bar)), "r"(parity)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(tc_smem_u32(bar)), "r"(parity)
+            : "memory");
+    return ok;
+}
+template <int nap, typename Attempt>
+__device__ __forceinline__ bool wg_wait_until(Attempt &&attempt, volatile int *abort_flag, unsigned int limit) {
     for (unsigned int spin = 0; spin < limit; ++spin) {
-        uint32_t ok;
-        if (kCluster)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                "selp.u32 %0, 1, 0, p;\n\t}"
-                : "=r"(ok)
-                : "r"(tc_smem_u32(bar)), "r"(parity)
-                : "memory");
-        else
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                "selp.u32 %0, 1, 0, p;\n\t}"
-                : "=r"(ok)
-                : "r"(tc_smem_u32(bar)), "r"(parity)
-                : "memory");
-        if (ok) return true;
+        if (attempt()) return true;
         if (nap > 0) __nanosleep(nap);
         if ((spin & 15u) == 15u && *abort_flag) return false;
     }
     *abort_flag = 1;
     return false;
 }
-// A warp's wait for one barrier, which every lane polls.
-template <int nap, bool kCluster = false>
-__device__ __forceinline__ bool wg_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
-    return __all_sync(0xFFFFFFFFu, wg_wait<nap, kCluster>(bar, parity, abort_flag, limit)) != 0;
+template <int nap>
+__device__ __forceinline__ bool wg_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
+    return wg_wait_until<nap>([&] { return wg_try(bar, parity) != 0u; }, abort_flag, limit);
 }
-// A warp's wait for barriers that its lanes poll side by side.  The vote orders no memory: what one lane's barrier guards, the others may read behind
-// the warp barrier only (492 -> 500 us at the size above).
-template <int nap, bool kCluster = false>
-__device__ __forceinline__ bool wg_wait_lanes(uint64_t *bar, uint32_t parity, volatile int *abort_flag, unsigned int limit) {
-    const bool ok = __all_sync(0xFFFFFFFFu, wg_wait<nap, kCluster>(bar, parity, abort_flag, limit)) != 0;
-    __syncwarp();
-    return ok;
+// A warp's wait for all barriers that `attempt` tries.  Every lane polls every one of them: a vote orders no memory, so that a lane may read
+// only what a barrier guards that it has polled itself.
+template <int nap, typename Attempt>
+__device__ __forceinline__ bool wg_wait_warp(Attempt &&attempt, volatile int *abort_flag, unsigned int limit) {
+    return __all_sync(0xFFFFFFFFu, wg_wait_until<nap>(attempt, abort_flag, limit)) != 0;
 }
 // One lane's arrival for its whole warp.
 __device__ __forceinline__ void wg_arrive_warp(uint64_t *bar) {
@@ -334,7 +335,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             for (int j = 0; j < 128; ++j) sum[j] = 0.f;
             for (int step = w.step0; step < w.step1; step += kWgChunkSteps, ++chain) {
                 const uint32_t buf = chain & 1u;
-                if (!wg_wait_warp<kWgNapEpilogue>(&sh.acc_full[buf], (chain >> 1) & 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                if (!wg_wait_warp<kWgNapEpilogue>([&] { return wg_try(&sh.acc_full[buf], (chain >> 1) & 1u) != 0u; }, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                 tc_fence_after_sync();
 #pragma unroll
                 for (int g = 0; g < 16; ++g) {
@@ -382,9 +383,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             // (a multiple of 4 tokens further on, a scale byte lies at the same place of its word)
             const int shift = ((row * a.blocks + w.m0 / kCodeBlock) & 3) * 8;
             for (int step = w.step0; step < w.step1; ++step) {
-                // (two lanes poll the codes' barrier and that of the place they go to)
-                if (!wg_wait_lanes<kWgNapWiden>(lane == 0 ? &sh.code_full[s] : &sh.done[o], lane == 0 ? full_phase : wide_phase, &sh.abort_flag,
-                                               a.spin_limit)) { alive = false; break; }
+                // (the codes, and the place they go to)
+                if (!wg_wait_warp<kWgNapWiden>([&] { const uint32_t x = wg_try(&sh.code_full[s], full_phase), y = wg_try(&sh.done[o], wide_phase); return (x & y) != 0u; },
+                                               &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                 const unsigned char *const codes = code_ring + s * kWgCodeBytes;
                 unsigned char *const wide = wide_ring + o * kWgWideBytes;
                 uint4 c[2 * kUnits];
@@ -452,8 +453,9 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
             __syncwarp();
         } else if (warp == 17) {
             // -------------------------------------------------------- MMA -------
-            // A wait costs some 250 clocks even when there is nothing to wait for: the barriers of a step are polled by three lanes at once.  The warp stays
-            // together (the MMAs' operands are in uniform registers then) and one elected lane issues.
+            // A wait costs some 250 clocks even when there is nothing to wait for, of which attempts issued one behind the other share most (three lanes that poll a
+            // barrier each, and meet at a warp barrier: 11.2 us at 300 x 768 x 768 instead of 10.3).  The warp stays together (the MMAs' operands are in uniform
+            // registers then) and one elected lane issues.
             int o = 0;
             uint32_t phase = 0, chain = 0;
             bool alive = true;
@@ -464,8 +466,11 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                     int in_chain = 0;
                     for (int step = w.step0; step < w.step1; ++step) {
                         const uint32_t buf = chain & 1u;
-                        if (in_chain == 0 && !wg_wait_warp<kWgNapMma, true>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
-                        if (!wg_wait_lanes<kWgNapMma, true>(lane == 0 ? &sh.dy_full[o] : lane == 1 ? &sh.wide_full[o] : &sh.other[o], phase, &sh.abort_flag, a.spin_limit)) {
+                        if (in_chain == 0 && !wg_wait_warp<kWgNapMma>([&] { return wg_try<true>(&sh.acc_empty[buf], ((chain >> 1) & 1u) ^ 1u) != 0u; }, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!wg_wait_warp<kWgNapMma>([&] {
+                                const uint32_t x = wg_try<true>(&sh.other[o], phase), y = wg_try(&sh.wide_full[o], phase), z = wg_try(&sh.dy_full[o], phase);
+                                return (x & y & z) != 0u;
+                            }, &sh.abort_flag, a.spin_limit)) {
                             alive = false;
                             break;
                         }
@@ -504,7 +509,8 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 for (int item = pair; item < a.items && alive; item += pairs) {
                     const WgItem w = wg_item(a, item, rank);
                     for (int step = w.step0; step < w.step1; ++step) {
-                        if (!wg_wait_lanes<kWgNapMma>(lane == 0 ? &sh.dy_full[o] : &sh.wide_full[o], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                        if (!wg_wait_warp<kWgNapMma>([&] { const uint32_t y = wg_try(&sh.wide_full[o], phase), z = wg_try(&sh.dy_full[o], phase); return (y & z) != 0u; },
+                                                     &sh.abort_flag, a.spin_limit)) { alive = false; break; }
                         tc_fence_async_smem();
                         wg_tell_first(&sh.told[o], &sh.other[o]);
                         if (++o == kWgRing) { o = 0; phase ^= 1u; }
@@ -552,7 +558,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
                 const int per_step = block < a.blocks ? kWgK * a.blocks : 0, per_row = per_step / kWgK;
                 for (int step = w.step0; step < w.step1; ++step) {
                     const int rows = block < a.blocks ? a.T - t_step * kWgK : 0;         // of the tokens that remain
-                    if (!wg_wait_warp<kWgNapCopy>(&sh.code_empty[s], phase, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
+                    if (!wg_wait_warp<kWgNapCopy>([&] { return wg_try(&sh.code_empty[s], phase) != 0u; }, &sh.abort_flag, a.spin_limit)) { alive = false; break; }
 #pragma unroll
                     for (int k = 0; k < kWgK / 32; ++k) {
                         const unsigned char *const word = from + 32 * k * per_row;

@@ -27,15 +27,14 @@ def calls(text, name):
         yield text[m.end():at - 1]
 
 
-def test_a_vote_over_different_barriers_is_followed_by_a_warp_barrier():
-    """Where the lanes of a warp wait for different barriers and vote, the vote orders no memory: a lane reads what another lane's barrier guards only
-    behind __syncwarp."""
+def test_every_lane_polls_every_barrier_that_it_waits_for():
+    """A vote orders no memory: where the lanes of a warp polled different barriers and voted, each could read only what its own one guards."""
     text = source("gaf_weight_grad.cuh")
-    different = [c for c in calls(text, "wg_wait_lanes") if "sh." in c]
-    assert len(different) == 3 and all("lane ==" in c for c in different)
-    assert not [c for c in calls(text, r"(?:wg_wait_warp|wg_wait)") if "lane" in c]
-    body = text[text.index("bool wg_wait_lanes"):]
-    assert re.match(r"[^}]*__all_sync\([^;]*;\s*__syncwarp\(\);\s*return", body)
+    waits = [c for c in calls(text, "wg_wait_warp") if "sh." in c]
+    assert len(waits) == 6 and not [c for c in waits if "lane" in c]
+    assert not [c for c in calls(text, "wg_try") if "lane" in c or "?" in c]
+    # (the one vote is that of wg_wait_warp)
+    assert len(re.findall(r"__all_sync|__any_sync|__ballot_sync", text)) == 1
 
 
 def test_what_passes_between_the_ctas_of_a_pair_is_ordered_at_cluster_scope():
@@ -47,9 +46,9 @@ def test_what_passes_between_the_ctas_of_a_pair_is_ordered_at_cluster_scope():
     assert remote and all(".cluster.shared::cluster" in r for r in remote)
     assert all("sh.other" in c for c in calls(text, r"(?<!void )wg_tell_first")) and "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes" in text
     assert all("sh.acc_empty" in c for c in calls(text, r"(?<!void )wg_arrive_warp_in_first"))
-    waits = re.findall(r"wg_wait\w*<[^<>]*>\([^;]*", text)
-    crossing = [w for w in waits if "sh.other" in w or "sh.acc_empty" in w]
-    assert len(crossing) == 2 and all(re.match(r"wg_wait\w*<\w+, true>", w) for w in crossing)
+    crossing = re.findall(r"wg_try\S*\(&sh\.(?:other|acc_empty)", text)
+    assert len(crossing) == 2 and all(c.startswith("wg_try<true>") for c in crossing)
+    assert text.count("acquire.cluster") == 1 and "acquire.cluster" in text[text.index("uint32_t wg_try"):text.index("bool wg_wait_until")]
 
 
 def test_every_variant_of_the_norm_is_one_that_some_width_takes():
