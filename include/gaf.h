@@ -138,7 +138,7 @@ enum {
     GAF_STATUS_ZERO_NORM = 1,   /* some tested pair had a zero norm (distance set to 1) */
     GAF_STATUS_NONFINITE = 2,   /* some sum was NaN or Inf */
     GAF_STATUS_TIMEOUT = 4,     /* a bounded wait inside a kernel (tensor-core Gram pipeline,
-                                   one-launch Gram-first schedule) ran out; the outputs of that
+                                   one-launch Gram-first schedule, weight gradient) ran out; the outputs of that
                                    call are not valid */
     GAF_STATUS_ILL_CONDITIONED = 8  /* after some accept the running sum g of the c accepted gradients
                                    had c * sum_i |g_i|^2 > 167 |g|^2: the accepted gradients nearly
@@ -379,7 +379,7 @@ int gaf_cosdist_static(const void *x, const void *y, int64_t D, int dtype,
  * Gradients of a language model's layers, written where the filter reads them
  * ---------------------------------------------------------------------------
  * The calls below make micro-gradients: the layers of a language model that are bound by memory, 8-bit
- * checkpoints of activations (K microbatches keep theirs until their backward passes), and the gradients that
+ * checkpoints of activations (what a forward pass has to keep for its backward pass), and the gradients that
  * read them.  A weight's gradient goes straight into its slice of the flat micro-gradient that
  * gaf_filter_accumulate takes (binary32 or bfloat16, `grad_dtype`), and is bitwise reproducible like the filter.
  * (The paper has no counterpart: its micro-gradients come out of a training framework.)
@@ -389,7 +389,9 @@ int gaf_cosdist_static(const void *x, const void *y, int64_t D, int dtype,
  *     4 binary32 or 8 bfloat16 elements), tokens to their own size.  Any T, d, stride is taken; rows that start on
  *     16-byte boundaries and are a multiple of 8 elements long are moved 16 bytes at a time.
  *   - `dtype` is the type of every matrix of a call and of the norm's weight.  Elements are computed, and sums
- *     carried, in binary32 or more, in an order that the sizes alone fix; each result is rounded once, to nearest.
+ *     carried, in binary32 or more; each result is rounded once, to nearest.  The order of every sum is fixed for the
+ *     same sizes, types, row distances, choice of a matrix or its checkpoint, and device: such calls give the same bits.  Another row distance
+ *     or another number of SMs may cut a sum differently.
  *   - `base` (of the gradient's type, may be NULL): what is added to a weight's gradient before it is rounded, for a
  *     weight that is used twice (an embedding table that is the output layer's weight too).  It may be the output itself.
  *   - Outputs must not overlap inputs or one another (GAF_ERR_ALIAS) except as said.

@@ -81,8 +81,10 @@ template <typename F> int by_flag(bool b, F &&f) { return b ? f(Flag<true>()) : 
 template <int N> struct Count { static constexpr int value = N; };
 
 // Threads per row and tiles per warp of the norm's kernels, by the width: as few threads as hold the row in registers.  The backward pass has
-// three times as much to hold and takes twice the threads (16384 x 4096 bfloat16: forward 95 us with 128 threads, 103 with 256;
-// backward from codes 105 and 95).
+// three times as much to hold and takes twice the threads.  As many threads / twice as many, us, L2 cold: forward, coded, bfloat16 16384 x 4096 96 / 98,
+// 8192 x 8192 98 / 115; backward from a matrix, bfloat16 106 / 100 and 106 / 98, binary32 8192 x 4096 100 / 102 and 4096 x 8192
+// 98 / 111; from codes, bfloat16 119 / 96 and 108 / 104, binary32 102 / 88 and 102 / 88.  (Beyond 8192 columns 512 threads with four tiles each
+// spill 320 to 512 bytes a thread.)
 template <bool BACKWARD, typename F>
 int by_width(int64_t d, F &&f) {
     if (d <= 256) return f(Count<32>(), Count<1>());
@@ -357,8 +359,9 @@ int gaf_embedding_grad(const void *dy, int64_t dy_stride, int64_t T, int64_t d, 
     a.dy_stride = dy_stride; a.V = V; a.T = T; a.d = d;
     a.tiles = ceil_div(d, kTile);
     a.scale = float(scale);
-    // few tokens for the table: filling is most of the work, and two CTAs of three do it (1000 tokens, 50,257 rows of 3 KB: 45.3 us with
-    // one, 34.9 with two)
+    // few tokens for the table: filling is most of the work, and two CTAs of three do it.  One / two, us, L2 cold: 50,257 rows of 3 KB, 1000 tokens
+    // 47 / 39, 3000 48 / 44, 6000 50 / 53, 9000 57 / 65, 16,384 72 / 82; 100,000 rows of 8 KB with a base, 4000 tokens 324 / 291, 11,000 322 / 318,
+    // 14,000 312 / 337, 32,768 331 / 452
     a.fillers = T < V / 8 ? 2 : 1;
     return launch_embedding_grad(a, dtype, grad_dtype, token_type, wide_rows(d, T, {dy_stride}), di, static_cast<cudaStream_t>(cuda_stream));
 }

@@ -3,7 +3,7 @@
 //     h = x + residual (rounded to the matrices' type)      r = 1 / sqrt(mean h^2 + eps)      y = h r w
 //     dx = residual_grad + r (w dy - h r^2 mean(w dy h))     dw = sum over rows of dy h r
 //
-// Both are bound by memory (16384 x 4096 bfloat16: forward with residual and coded result 97 us, 6.2 TB/s; backward from an 8-bit checkpoint with a
+// Both are bound by memory (16384 x 4096 bfloat16: forward with residual and coded result 96 to 100 us, 6.0 to 6.3 TB/s, with h's checkpoint too 113 us; backward from an 8-bit checkpoint with a
 // residual's gradient 90 us, 5.2 TB/s, issue slots half taken).  A row is held in registers between its reduction and its results, so that everything is read and
 // written once: R threads of a CTA share a row, up to S tiles of 256 columns per warp.
 #pragma once
@@ -154,8 +154,8 @@ __global__ void __launch_bounds__(norm_threads(R)) rms_norm_grad_kernel(const __
         const int64_t c = (int64_t)(s * (R / 32) + w_row) * kTile;
         load_tile<VEC>(static_cast<const T *>(a.weight) + c, lane, a.d - c, s_w[s]);
     }
-    // the next row in flight while this one is summed and written: not in binary32, whose rows take all registers (16384 x 4096: 165 us without,
-    // 185 us with; bfloat16 85 and 76 us)
+    // the next row in flight while this one is summed and written: not in binary32, whose rows take all registers (16384 x 4096, without a
+    // residual's gradient: 142 us; with the next row in flight it was 185 against 165 us, in bfloat16 76 against 85 us)
     constexpr bool kAhead = sizeof(T) == 2;
     if (kAhead) load(row);
     int turn = 0;

@@ -13,9 +13,10 @@
 // 1024 clocks of the tensor core, an SM's shared memory takes in 48 KB of copies, is read for 16 KB and written 32 KB by widening, and read for
 // 64 KB by the MMAs: 160 of the 128 bytes a clock that it has, so that the tensor cores cannot be busy for more than four fifths of the time.
 //
-// Measured at T = 16384, N = M = 4096, dW in binary32: 480 us with random data (1.14 PFLOP/s, 0.68 of the measured cuBLAS burst, 0.82 of
-// its rate under the power limit), 421 us in short runs; tensor pipe active 71 % of the
-// cycles.  T = 300, N = M = 768: 10.7 us, two launches.
+// Measured at T = 16384, N = M = 4096, dW in binary32: 463 us with random data (1.19 PFLOP/s, 0.71 of the measured cuBLAS burst, 0.85 of
+// its rate under the power limit), 381 us in short runs; tensor pipe active 78 % of the
+// cycles.  T = 300, N = M = 768: 10.2 us, two launches.  T = 4096, N = M = 4096: 118 us, with binary32 dy (three terms) 366 us.  T = 4096,
+// N = 50,257, M = 768: 278 us in aligned rows, 1146 us in dense ones, which are laid out anew first.
 //
 // Accuracy.  A tensor core adds to its binary32 accumulator by cutting off, not by rounding; over many steps that pulls a sum
 // towards zero.  A chain therefore ends after kWgChunk tokens, and the chains are added, rounded to nearest, in registers of the epilogue's

@@ -229,9 +229,9 @@ class LanguageModel:
         return t
 
     def micro_gradient(self, tokens: torch.Tensor, targets: torch.Tensor, flat: torch.Tensor, workspace: torch.Tensor) -> dict:
-        """Forward and backward pass of one microbatch: the gradient into ``flat`` (float32 or bfloat16, all slices written).  Between the
-        passes only 8-bit checkpoints of the activations are kept.  Returns the activations and their gradients by name (for
-        tests: a training step has no use for them)."""
+        """Forward and backward pass of one microbatch: the gradient into ``flat`` (float32 or bfloat16, all slices written).  The backward
+        pass reads of the forward one the 8-bit checkpoints, the roots and the logits' gradient.  Returns the activations and their gradients by
+        name, for tests (which keeps them all alive: a training step would let each go after its last use)."""
         from . import binding as gaf
         g, T, scale = self.views(flat), tokens.numel(), math.sqrt(self.d)
         y1c, h1c, y2c, h2c = (gaf.new_checkpoint(T, self.d, self.device) for _ in range(4))
