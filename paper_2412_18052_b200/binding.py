@@ -274,7 +274,8 @@ def new_layer_workspace(T: int, width: int, dtype: int, V: int = 0, device=None)
     (``dtype``: GAF_F32 if any gradient call has float32 matrices).  Its contents do not matter to any result; it is prepared by
     gaf_workspace_init all the same, for its status and for the filter, which it serves too if it is large enough."""
     ws = torch.empty(gaf_layer_workspace_bytes(T, width, dtype, V), dtype=torch.uint8, device=device or "cuda")
-    gaf_workspace_init(ws)
+    with torch.cuda.device(ws.device):                          # (its stream: another device may be the current one)
+        gaf_workspace_init(ws)
     return ws
 
 
