@@ -191,7 +191,7 @@ __device__ __forceinline__ void wg_arrive_warp_in_first(uint64_t *bar) {
         "@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(wg_in_first(bar)) : "memory");
 }
 // One lane tells the first CTA what this CTA has in shared memory: a word stored there asynchronously, whose 4 bytes complete the barrier's phase with
-// release semantics at cluster scope.  (An arrival with release semantics takes hundreds of clocks a step: 581 us against 488 at the size above.)
+// release semantics at cluster scope.  (An arrival with release semantics takes hundreds of clocks a step: 581 us where this took 488, at the size above, before the waits became what they are.)
 __device__ __forceinline__ void wg_tell_first(uint32_t *word, uint64_t *bar) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -455,7 +455,7 @@ weight_grad_kernel(const __grid_constant__ WeightGradArgs a, const __grid_consta
         } else if (warp == 17) {
             // -------------------------------------------------------- MMA -------
             // A wait costs some 250 clocks even when there is nothing to wait for, of which attempts issued one behind the other share most (three lanes that poll a
-            // barrier each, and meet at a warp barrier: 11.2 us at 300 x 768 x 768 instead of 10.3).  The warp stays together (the MMAs' operands are in uniform
+            // barrier each, and meet at a warp barrier: 11.2 us at 300 x 768 x 768 instead of 10.2).  The warp stays together (the MMAs' operands are in uniform
             // registers then) and one elected lane issues.
             int o = 0;
             uint32_t phase = 0, chain = 0;
